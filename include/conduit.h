@@ -435,6 +435,181 @@ conduit_status conduit_residual_error(const conduit_kv *kv, const void *q, int32
                                       float kappa, float *err_out, void *ws, size_t ws_bytes,
                                       hipStream_t stream);
 
+/* ------------------------------------------------------------------------ *
+ * Rotary positions with several axes (time, height, width, ...; one axis for
+ * text).  Frequency f (0 <= f < rot_dim / 2) turns one pair (a, b) of every
+ * head by theta = inv_freq[f] * p, p the row's position on axis[f]:
+ *     a' = a cos(theta) - b sin(theta),   b' = a sin(theta) + b cos(theta).
+ * The pair of f is (f, f + rot_dim / 2) with CONDUIT_PAIR_HALVES and (2f, 2f + 1)
+ * with CONDUIT_PAIR_ADJACENT; dims from rot_dim on pass through.  Angles, sines,
+ * cosines and the turn are computed in 64 bits, the result is rounded to fp32
+ * and then to the tensor's dtype.  A factor on cosine and sine (as some context
+ * extensions use) belongs into the attention's scale instead.
+ * HOST memory, read during the call only (a captured call keeps what it read).
+ * ------------------------------------------------------------------------ */
+#define CONDUIT_MAX_AXES 4
+#define CONDUIT_ROTARY_MAX_DIM 256
+
+typedef enum { CONDUIT_PAIR_HALVES = 0, CONDUIT_PAIR_ADJACENT = 1 } conduit_pairing;
+
+typedef struct {
+  int32_t rot_dim;        /* dims that turn: even, 2 .. head_dim                     */
+  int32_t n_axes;         /* 1 .. CONDUIT_MAX_AXES                                   */
+  int32_t pairing;        /* conduit_pairing                                         */
+  const float *inv_freq;  /* HOST [rot_dim / 2]: radians per position, finite,
+                             magnitude <= 1024                                       */
+  const int32_t *axis;    /* HOST [rot_dim / 2]: the axis of each frequency, in
+                             [0, n_axes); NULL: axis 0 for all                       */
+} conduit_rope;
+
+/* ------------------------------------------------------------------------ *
+ * Turns the heads of n rows (queries, keys or their gradients).
+ *
+ * x, out    device rows of n_heads dense heads of head_dim, x_stride / out_stride
+ *           elements apart (>= n_heads * head_dim, multiples of 16 bytes; below
+ *           32 MiB).  out may be x with the same stride (in place); any other
+ *           overlap is not allowed.
+ * head_dim  a multiple of 8 up to CONDUIT_ROTARY_MAX_DIM.
+ * rope_pos  device int32 [n_axes][n], any value, axis a at
+ *           rope_pos + a * rope_pos_stride (rope_pos_stride >= n).
+ * inverse   0, or 1 to turn by -theta: the inverse of the turn and, the turn
+ *           being orthogonal, its gradient (x: the output's gradient, out: the
+ *           input's).
+ * n = 0 enqueues nothing.
+ * ------------------------------------------------------------------------ */
+conduit_status conduit_rotary(const void *x, int64_t x_stride, int32_t n, int32_t n_heads, int32_t head_dim,
+                              int32_t dtype, const conduit_rope *rope, const int32_t *rope_pos,
+                              int64_t rope_pos_stride, int32_t inverse, void *out, int64_t out_stride,
+                              hipStream_t stream);
+
+/* New tokens of one layer, as the projections leave them: rows of n_kv_heads
+ * dense key heads, value heads and, when q is given, n_q_heads query heads, each
+ * with its own row stride (slices of one fused buffer will do).  16-byte
+ * aligned; strides multiples of 16 bytes and below 32 MiB. */
+typedef struct {
+  int32_t n;              /* rows                                                    */
+  int32_t dtype;          /* conduit_dtype of k, v, q and q_out                      */
+  const void *k;          /* device [n][n_kv_heads][head_dim]                        */
+  const void *v;          /* device, same layout                                     */
+  int64_t k_stride;       /* elements between rows                                   */
+  int64_t v_stride;
+  const void *q;          /* nullable: device [n][n_q_heads][head_dim]               */
+  void *q_out;            /* the turned queries (with q; may be q, with its stride)  */
+  int64_t q_stride;
+  int64_t q_out_stride;
+} conduit_rows;
+
+/* ------------------------------------------------------------------------ *
+ * Appends (or overwrites) rows of a cache: row i's keys, turned by rope, and its
+ * values become token pos[i] of kv; its queries, turned likewise, go to q_out.
+ *
+ * pos       device int32 [n].  A row whose position is outside [0, kv->n_ctx)
+ *           leaves the cache as it was (padded rows: -1); its q_out is still
+ *           written.  Positions that two rows share receive a mixture of the
+ *           two rows.
+ *           A batch over one page pool is the pool taken as a contiguous
+ *           cache of n_pages * page_size tokens, pos holding pool rows.
+ * rows      dtype that of kv; must not overlap the cache (q_out may be q).
+ * rope, rope_pos, rope_pos_stride  as in conduit_rotary, rot_dim a multiple of 16
+ *           (CONDUIT_ERR_UNSUPPORTED otherwise); rope NULL: nothing turns.
+ * n = 0 enqueues nothing.
+ * ------------------------------------------------------------------------ */
+conduit_status conduit_append_kv(const conduit_kv *kv, const conduit_rows *rows, const int32_t *pos,
+                                 const conduit_rope *rope, const int32_t *rope_pos, int64_t rope_pos_stride,
+                                 hipStream_t stream);
+
+/* One layer's KV cache in 4 bits, for one or more sequences (microscaling fp4).
+ *
+ * 32 consecutive dims of one token and head share a scale byte s and hold codes
+ * of 4 bits: sign, and the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6.  A value is
+ * code * 2^(s - 127), exact in bf16.  Written blocks take the smallest s (kept in
+ * [2, 252]) with max|x| <= 6 * 2^(s - 127), so that no code saturates below
+ * 1.5 * 2^127, and the nearest codes, ties to the even code; x is the row as a
+ * cache of rows->dtype would hold it.  A token that has an infinity or a NaN
+ * among its keys or values of some head is stored with scale byte 255 (NaN) in
+ * that head's keys and zero values: rows that attend to it are NaN there.
+ *
+ * Pools: page p holds [n_kv_heads][page_size][head_dim / 2] code bytes (dim 2i in
+ * the low four bits) at k + p * code_stride, and [n_kv_heads][page_size]
+ * [head_dim / 32] scale bytes at k_scale + p * scale_stride; v likewise.
+ * Token t of sequence s is slot t % page_size of page
+ * block_table[s * table_stride + t / page_size], or, without a table, of page
+ * s * table_stride + t / page_size.  Entries outside [0, n_pages) are clamped
+ * into it (the results are then meaningless, but no access leaves the pool).
+ * Pages may be shared between sequences (a reused image) or unused. */
+typedef struct {
+  void *k;                /* device code bytes, 16-byte aligned                      */
+  void *v;
+  void *k_scale;          /* device scale bytes, 16-byte aligned                     */
+  void *v_scale;
+  int64_t code_stride;    /* bytes between pages of k and of v: a multiple of 16,
+                             >= n_kv_heads * page_size * head_dim / 2                */
+  int64_t scale_stride;   /* the same for k_scale and v_scale                        */
+  int32_t n_pages;        /* pages in each pool                                      */
+  int32_t page_size;      /* tokens per page: a power of two from 64 to 2^20         */
+  int32_t n_seqs;         /* sequences                                               */
+  int32_t table_stride;   /* pages of a sequence                                     */
+  int32_t n_ctx;          /* tokens a sequence holds: 1 .. table_stride * page_size  */
+  const int32_t *block_table; /* device [n_seqs][table_stride], or NULL              */
+  int32_t n_q_heads;      /* a multiple of n_kv_heads                                */
+  int32_t n_kv_heads;     /* up to 256                                               */
+  int32_t head_dim;       /* 64 or 128                                               */
+} conduit_kv_mx;
+
+/* ------------------------------------------------------------------------ *
+ * conduit_append_kv into a 4-bit cache.  Rows are shared out evenly over the
+ * sequences: row i is token pos[i] of sequence i / (n / n_seqs), and n must be a
+ * multiple of n_seqs.  Rows may be bf16 or fp32.
+ *
+ * k_out, v_out  nullable device [n][n_kv_heads][head_dim] dense, rows->dtype: the
+ *           keys and values as the cache holds them (for every row, also those
+ *           that pos leaves out).
+ * ------------------------------------------------------------------------ */
+conduit_status conduit_append_mx(const conduit_kv_mx *mx, const conduit_rows *rows, const int32_t *pos,
+                                 const conduit_rope *rope, const int32_t *rope_pos, int64_t rope_pos_stride,
+                                 void *k_out, void *v_out, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * Loads rows of a 4-bit cache into a cache of 16 or 32 bits: token src_pos[i] of
+ * sequence i / (n / n_seqs) of mx becomes token dst_pos[i] of kv, its keys turned
+ * by rope (rope_pos then holds how far the row moves on each axis; NULL: keys
+ * keep their positions).  A row with src_pos outside [0, mx->n_ctx) or dst_pos
+ * outside [0, kv->n_ctx) leaves kv as it was.  kv and mx have the same
+ * n_kv_heads and head_dim; dst_pos holds no position twice.
+ * ------------------------------------------------------------------------ */
+conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, int32_t n, const conduit_kv *kv,
+                               const int32_t *dst_pos, const conduit_rope *rope, const int32_t *rope_pos,
+                               int64_t rope_pos_stride, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * Causal attention over a 4-bit cache: one generated token of each sequence, a
+ * few drafted ones, or the selected rows of a refresh.  Row i belongs to
+ * sequence i / (n / n_seqs) (n a multiple of n_seqs) and attends to that
+ * sequence's keys 0 .. pos[i].
+ *
+ * q         device [n][n_q_heads][head_dim] dense, dtype: CONDUIT_BF16, or
+ *           CONDUIT_F32 (queries and probabilities then enter the matrix
+ *           products in three exact bf16 parts, so that nothing is rounded
+ *           below fp32).
+ * pos       device int32 [n].  Below 0: the row attends to nothing, its output
+ *           is 0 and its log-sum-exp -inf (padded rows).  Positions from n_ctx on
+ *           read no key past n_ctx - 1 (the row's output is then meaningless).
+ *           Keys past a row's position do not enter its output, whatever they
+ *           hold.
+ * o_out     device [n][n_q_heads][head_dim], dtype.
+ * lse_out   nullable device [n][n_q_heads] fp32: natural-log log-sum-exp.
+ * ws        conduit_attn_mx_workspace_bytes(mx, n, dtype) bytes, 256-byte aligned
+ *           (0 bytes: may be NULL).  Needs no initialisation; a captured call
+ *           may share it with others that do not run at the same time.
+ * Errors: CONDUIT_ERR_UNSUPPORTED if n * n_q_heads exceeds 2^24.
+ * n = 0 enqueues nothing.
+ * ------------------------------------------------------------------------ */
+size_t conduit_attn_mx_workspace_bytes(const conduit_kv_mx *mx, int32_t n, int32_t dtype);
+
+conduit_status conduit_attn_mx(const conduit_kv_mx *mx, const void *q, int32_t dtype, const int32_t *pos, int32_t n,
+                               float scale, void *o_out, float *lse_out, void *ws, size_t ws_bytes,
+                               hipStream_t stream);
+
 /* ------------------------------------------------------------------------
  * Kernel timing, a tracing aid.  While enabled on the calling thread, every
  * kernel launch made by the entry points above is bracketed by two HIP

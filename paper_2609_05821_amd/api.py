@@ -23,7 +23,9 @@ F32, BF16 = 0, 1
 NORM_CAUSAL_ROW, NORM_VISUAL_ONLY = 0, 1
 AGG_MEAN, AGG_RMS = 0, 1
 RANK_COMPOSITE, RANK_ATTENTION, RANK_EXPLICIT = 0, 1, 2
+PAIR_HALVES, PAIR_ADJACENT = 0, 1
 MAX_IMAGES = 256
+MAX_AXES = 4
 
 EXPORTS = [
     "conduit_budget", "conduit_score_workspace_bytes", "conduit_score",
@@ -34,6 +36,8 @@ EXPORTS = [
     "conduit_residual_error", "conduit_score_noalloc", "conduit_scatter_kv_layers",
     "conduit_refresh_layers_workspace_bytes", "conduit_refresh_attn_layers",
     "conduit_score_layers_workspace_bytes", "conduit_score_layers", "conduit_merge_refresh_attn",
+    "conduit_rotary", "conduit_append_kv", "conduit_append_mx", "conduit_load_mx",
+    "conduit_attn_mx_workspace_bytes", "conduit_attn_mx",
 ]
 SCORE_NOALLOC_MAX_BYTES = 16 << 20
 
@@ -57,6 +61,25 @@ class Images(ctypes.Structure):
     _fields_ = [("n_images", ctypes.c_int32), ("n_vis", ctypes.c_int32),
                 ("img_pos", ctypes.POINTER(ctypes.c_int32)),
                 ("img_off", ctypes.POINTER(ctypes.c_int32))]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("inv_freq", ctypes.POINTER(ctypes.c_float)), ("axis", ctypes.POINTER(ctypes.c_int32))]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("dtype", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64)]
+
+
+class KVMX(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("code_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32), ("n_ctx", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 _lib = None
@@ -114,6 +137,19 @@ def lib() -> ctypes.CDLL:
         L.conduit_score_layers.argtypes = [pkv, i32, pvp, i32, i32, pimg, ctypes.c_int, ctypes.c_int, f32, pvp,
                                            vp, vp, i32, vp, sz, vp]
         L.conduit_score_layers.restype = ctypes.c_int
+        prope, prows, pmx = ctypes.POINTER(RopeDesc), ctypes.POINTER(Rows), ctypes.POINTER(KVMX)
+        L.conduit_rotary.argtypes = [vp, i64, i32, i32, i32, i32, prope, vp, i64, i32, vp, i64, vp]
+        L.conduit_rotary.restype = ctypes.c_int
+        L.conduit_append_kv.argtypes = [pkv, prows, vp, prope, vp, i64, vp]
+        L.conduit_append_kv.restype = ctypes.c_int
+        L.conduit_append_mx.argtypes = [pmx, prows, vp, prope, vp, i64, vp, vp, vp]
+        L.conduit_append_mx.restype = ctypes.c_int
+        L.conduit_load_mx.argtypes = [pmx, vp, i32, pkv, vp, prope, vp, i64, vp]
+        L.conduit_load_mx.restype = ctypes.c_int
+        L.conduit_attn_mx_workspace_bytes.argtypes = [pmx, i32, i32]
+        L.conduit_attn_mx_workspace_bytes.restype = sz
+        L.conduit_attn_mx.argtypes = [pmx, vp, i32, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.conduit_attn_mx.restype = ctypes.c_int
         L.conduit_status_str.argtypes = [ctypes.c_int]
         L.conduit_status_str.restype = ctypes.c_char_p
         L.conduit_last_error.argtypes = []
@@ -406,6 +442,208 @@ def conduit_merge_refresh_attn(kv: KV, pos: torch.Tensor, k_new: torch.Tensor, v
     _check(lib().conduit_merge_refresh_attn(ctypes.byref(kv), pos.data_ptr(), k, k_new.data_ptr(), v_new.data_ptr(),
                                             q_sel.data_ptr(), scale, o_out.data_ptr(), _ptr(lse_out), _ptr(ws),
                                             _nbytes(ws), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# Positions, growing caches, 4-bit caches
+# ---------------------------------------------------------------------------
+
+class Rope:
+    """Rotary frequencies (conduit_rope), host arrays kept alive for the calls.
+
+    inv_freq: radians per position of the rot_dim / 2 frequencies; axis: the
+    position axis of each (None: one axis).  With time, height and width in
+    sections of 16, 24 and 24 frequencies, axis is [0] * 16 + [1] * 24 + [2] * 24;
+    an interleaved order is any other list."""
+
+    def __init__(self, inv_freq: Sequence[float], axis: Optional[Sequence[int]] = None,
+                 n_axes: Optional[int] = None, pairing: int = PAIR_HALVES):
+        self.inv_freq = np.array(inv_freq, dtype=np.float32, order="C")
+        self.axis = None if axis is None else np.array(axis, dtype=np.int32, order="C")
+        if self.inv_freq.ndim != 1 or (self.axis is not None and self.axis.shape != self.inv_freq.shape):
+            raise ConduitError(ERR_INVALID_ARG, "inv_freq and axis must be flat and of one length")
+        if n_axes is None:
+            n_axes = 1 if self.axis is None or self.axis.size == 0 else int(self.axis.max()) + 1
+        self.desc = RopeDesc(2 * self.inv_freq.size, n_axes, pairing,
+                             self.inv_freq.ctypes.data_as(ctypes.POINTER(ctypes.c_float)),
+                             None if self.axis is None else
+                             self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)))
+
+    @property
+    def n_axes(self) -> int:
+        return int(self.desc.n_axes)
+
+
+def mx_desc(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, n_q_heads: int,
+            n_ctx: Optional[int] = None, block_table: Optional[torch.Tensor] = None, n_seqs: int = 1) -> KVMX:
+    """Descriptor of one layer's 4-bit cache: k, v uint8 [n_pages, H_kv, page, d / 2]
+    codes, k_scale, v_scale uint8 [n_pages, H_kv, page, d / 32] (pages evenly
+    strided, dense inside).  block_table: device int32 [n_seqs, pages] of the
+    sequences' pages, or None, when the pool's pages belong to n_seqs sequences
+    in order.  n_ctx: tokens a sequence holds (default: all its pages)."""
+    for t in (k, v, k_scale, v_scale):
+        if t.dtype != torch.uint8 or t.dim() != 4 or not t[:1].is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "pools must be uint8 [n_pages, H_kv, page, bytes], pages dense")
+    n_pages, hkv, page, half = k.shape
+    if v.shape != k.shape or v_scale.shape != k_scale.shape or k_scale.shape != (n_pages, hkv, page, half // 16) or \
+            half % 16:
+        raise ConduitError(ERR_INVALID_ARG, "the pools' shapes do not belong together")
+    if n_pages > 1 and (k.stride(0) != v.stride(0) or k_scale.stride(0) != v_scale.stride(0)):
+        raise ConduitError(ERR_INVALID_ARG, "k and v (and their scales) must have one page stride")
+    if block_table is not None:
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "block_table must be int32 [n_seqs, pages], dense")
+        n_seqs, table_stride = block_table.shape
+    else:
+        table_stride = n_pages // max(n_seqs, 1)
+    _one_device(k, v, k_scale, v_scale, block_table)
+    code_stride = k.stride(0) if n_pages > 1 else hkv * page * half
+    scale_stride = k_scale.stride(0) if n_pages > 1 else hkv * page * (half // 16)
+    return KVMX(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), code_stride, scale_stride, n_pages,
+                page, n_seqs, table_stride, table_stride * page if n_ctx is None else n_ctx, _ptr(block_table),
+                n_q_heads, hkv, 2 * half)
+
+
+def _one_device(*tensors) -> Optional[torch.device]:
+    devs = {t.device for t in tensors if t is not None}
+    if len(devs) > 1:
+        raise ConduitError(ERR_INVALID_ARG, f"tensors on different devices: {sorted(map(str, devs))}")
+    return devs.pop() if devs else None
+
+
+def _call(fn, tensors, stream, *args) -> None:
+    """fn(*args, stream) with the tensors' device current: one device for all, the
+    current stream of that device unless one is given."""
+    dev = _one_device(*tensors)
+    if dev is None or dev.type != "cuda":
+        raise ConduitError(ERR_INVALID_ARG, "tensors must be on the GPU")
+    if stream is not None and stream.device != dev:
+        raise ConduitError(ERR_INVALID_ARG, f"stream of {stream.device} for tensors on {dev}")
+    with torch.cuda.device(dev):
+        _check(fn(*args, (stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream))
+
+
+def _heads(t: torch.Tensor, what: str) -> int:
+    """Row stride of [n, H, d] with dense heads (any row stride)."""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] != 1 and t.stride(1) != t.shape[2]):
+        raise ConduitError(ERR_INVALID_ARG, f"{what} must be [n, H, d] with dense heads")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _row_ids(t: torch.Tensor, n: int, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ConduitError(ERR_INVALID_ARG, f"{what} must be dense int32 [{n}]")
+    return t
+
+
+def _rope_args(rope: Optional[Rope], rope_pos: Optional[torch.Tensor], n: int):
+    """(descriptor, positions, stride) of n rows; rope_pos [n_axes, n], or [n] for one axis."""
+    if (rope is None) != (rope_pos is None):
+        raise ConduitError(ERR_INVALID_ARG, "rope and rope_pos go together")
+    if rope is None:
+        return None, None, 0
+    if rope_pos.dim() == 1:
+        rope_pos = rope_pos[None]
+    if rope_pos.dtype != torch.int32 or rope_pos.shape != (rope.n_axes, n) or (n > 1 and rope_pos.stride(1) != 1):
+        raise ConduitError(ERR_INVALID_ARG, f"rope_pos must be int32 [{rope.n_axes}, {n}], rows dense")
+    return ctypes.byref(rope.desc), rope_pos.data_ptr(), max(rope_pos.stride(0), n)
+
+
+def conduit_rotary(x: torch.Tensor, rope: Rope, rope_pos: torch.Tensor, out: torch.Tensor, inverse: bool = False,
+                   stream=None) -> None:
+    """out = the heads of x [n, H, d] turned by their rows' positions (out may be x);
+    with inverse turned back, which is also the gradient; see conduit_rotary in
+    conduit.h."""
+    xs, os_ = _heads(x, "x"), _heads(out, "out")
+    if x.shape != out.shape or x.dtype != out.dtype:
+        raise ConduitError(ERR_INVALID_ARG, "x and out must match in shape and dtype")
+    n, heads, d = x.shape
+    desc, pos, ps = _rope_args(rope, rope_pos, n)
+    _call(lib().conduit_rotary, (x, out, rope_pos), stream, _ptr(x), xs, n, heads, d, _dtype_code(x), desc, pos, ps,
+          int(inverse), _ptr(out), os_)
+
+
+def _new_rows(k_new, v_new, q, q_out, n_q_heads: int, n_kv_heads: int, d: int) -> Rows:
+    n = k_new.shape[0]
+    ks, vs = _heads(k_new, "k_new"), _heads(v_new, "v_new")
+    if k_new.shape != (n, n_kv_heads, d) or v_new.shape != k_new.shape:
+        raise ConduitError(ERR_INVALID_ARG, f"k_new and v_new must be [n, {n_kv_heads}, {d}]")
+    if (q is None) != (q_out is None):
+        raise ConduitError(ERR_INVALID_ARG, "q and q_out go together")
+    if any(t is not None and t.dtype != k_new.dtype for t in (v_new, q, q_out)):
+        raise ConduitError(ERR_INVALID_ARG, "k_new, v_new, q and q_out must have one dtype")
+    qs = qos = 0
+    if q is not None:
+        qs, qos = _heads(q, "q"), _heads(q_out, "q_out")
+        if q.shape != (n, n_q_heads, d) or q_out.shape != q.shape:
+            raise ConduitError(ERR_INVALID_ARG, f"q and q_out must be [n, {n_q_heads}, {d}]")
+    return Rows(n, _dtype_code(k_new), _ptr(k_new), _ptr(v_new), ks, vs, _ptr(q), _ptr(q_out), qs, qos)
+
+
+def conduit_append_kv(kv: KV, pos: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                      rope: Optional[Rope] = None, rope_pos: Optional[torch.Tensor] = None,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """New tokens into a cache, keys (and queries) turned on the way; see
+    conduit_append_kv.  k_new, v_new [n, H_kv, d], q, q_out [n, H_q, d] with any
+    row stride; pos int32 [n], outside the cache: the row is left out."""
+    rows = _new_rows(k_new, v_new, q, q_out, kv.n_q_heads, kv.n_kv_heads, kv.head_dim)
+    desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
+    _call(lib().conduit_append_kv, (k_new, v_new, q, q_out, _row_ids(pos, rows.n, "pos"), rope_pos), stream,
+          ctypes.byref(kv), ctypes.byref(rows), _ptr(pos), desc, rp, ps)
+
+
+def conduit_append_mx(mx: KVMX, pos: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                      rope: Optional[Rope] = None, rope_pos: Optional[torch.Tensor] = None,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                      k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """New tokens into a 4-bit cache (row i to sequence i // (n / n_seqs)); k_out,
+    v_out [n, H_kv, d] receive the rows as the cache holds them; see
+    conduit_append_mx."""
+    rows = _new_rows(k_new, v_new, q, q_out, mx.n_q_heads, mx.n_kv_heads, mx.head_dim)
+    for t in (k_out, v_out):
+        if t is not None and (t.shape != k_new.shape or t.dtype != k_new.dtype or not t.is_contiguous()):
+            raise ConduitError(ERR_INVALID_ARG, "k_out and v_out must be dense and shaped like k_new")
+    desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
+    _call(lib().conduit_append_mx, (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), rope_pos),
+          stream, ctypes.byref(mx), ctypes.byref(rows), _ptr(pos), desc, rp, ps, _ptr(k_out), _ptr(v_out))
+
+
+def conduit_load_mx(mx: KVMX, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tensor, rope: Optional[Rope] = None,
+                    rope_pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows of a 4-bit cache into a 16- or 32-bit cache, keys turned by how far they
+    move (rope_pos [n_axes, n]); see conduit_load_mx."""
+    n = src_pos.numel()
+    desc, rp, ps = _rope_args(rope, rope_pos, n)
+    _call(lib().conduit_load_mx, (_row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos"), rope_pos), stream,
+          ctypes.byref(mx), _ptr(src_pos), n, ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
+
+
+def attn_mx_workspace_bytes(mx: KVMX, q: torch.Tensor) -> int:
+    return int(lib().conduit_attn_mx_workspace_bytes(ctypes.byref(mx), q.shape[0], _dtype_code(q)))
+
+
+def conduit_attn_mx(mx: KVMX, q: torch.Tensor, pos: torch.Tensor, o_out: torch.Tensor,
+                    lse_out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                    ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal attention of rows over a 4-bit cache: q, o_out dense [n, H_q, d], pos
+    int32 [n] (below 0: an empty row), lse_out fp32 [n, H_q]; see conduit_attn_mx."""
+    n = q.shape[0]
+    if q.shape != (n, mx.n_q_heads, mx.head_dim) or o_out.shape != q.shape or o_out.dtype != q.dtype or \
+            not q.is_contiguous() or not o_out.is_contiguous():
+        raise ConduitError(ERR_INVALID_ARG, f"q and o_out must be dense [n, {mx.n_q_heads}, {mx.head_dim}] of one dtype")
+    if lse_out is not None and (lse_out.shape != q.shape[:2] or lse_out.dtype != torch.float32 or
+                                not lse_out.is_contiguous()):
+        raise ConduitError(ERR_INVALID_ARG, "lse_out must be dense float32 [n, H_q]")
+    if scale is None:
+        scale = 1.0 / math.sqrt(mx.head_dim)
+    need = attn_mx_workspace_bytes(mx, q)
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if stream is not None:
+            ws.record_stream(stream)  # freed on return, used on that stream
+    _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws), stream, ctypes.byref(mx), _ptr(q),
+          _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
 
 
 def profile_enable(enabled: bool) -> None:

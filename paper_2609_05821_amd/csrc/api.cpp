@@ -12,6 +12,7 @@
 #include <string>
 
 #include "common.h"
+#include "mx.h"
 
 using namespace conduit;
 
@@ -1192,6 +1193,323 @@ conduit_status conduit_refresh_attn_layers(const conduit_kv *kvs, int32_t n_laye
     const hipError_t e = launch_attn(ap, kv->head_dim, true, stream, &lt, l0 > 0);
     if (e != hipSuccess) return hip_fail(e, "refresh attention");
   }
+  return ok();
+}
+
+namespace {
+
+// The rope's table for kernel arguments; half = 0 (nothing turns) without one.
+// turn_multiple: what rot_dim has to be a multiple of (2: any even).
+conduit_status rope_table(const conduit_rope *rope, const int32_t *rope_pos, int64_t rope_pos_stride, int32_t n,
+                          int32_t head_dim, int32_t inverse, int32_t turn_multiple, RopeTable *t) {
+  memset(t, 0, sizeof(*t));
+  if (!rope) return CONDUIT_OK;
+  if (rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > head_dim)
+    return fail(CONDUIT_ERR_INVALID_ARG, "rot_dim %d is not even in [2, head_dim = %d]", rope->rot_dim, head_dim);
+  if (rope->rot_dim % turn_multiple)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "rot_dim %d (supported here: multiples of %d)", rope->rot_dim, turn_multiple);
+  if (rope->n_axes < 1 || rope->n_axes > CONDUIT_MAX_AXES)
+    return fail(CONDUIT_ERR_INVALID_ARG, "n_axes = %d outside [1, %d]", rope->n_axes, CONDUIT_MAX_AXES);
+  if (rope->pairing != CONDUIT_PAIR_HALVES && rope->pairing != CONDUIT_PAIR_ADJACENT)
+    return fail(CONDUIT_ERR_INVALID_ARG, "pairing %d is not a conduit_pairing", rope->pairing);
+  if (!rope->inv_freq) return fail(CONDUIT_ERR_INVALID_ARG, "inv_freq is NULL");
+  if (!rope_pos || reinterpret_cast<uintptr_t>(rope_pos) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "rope_pos must be non-NULL and 4-byte aligned");
+  if (rope->n_axes > 1 && rope_pos_stride < n)
+    return fail(CONDUIT_ERR_INVALID_ARG, "rope_pos_stride %lld below the %d rows", (long long)rope_pos_stride, n);
+  t->half = rope->rot_dim / 2;
+  t->adjacent = rope->pairing == CONDUIT_PAIR_ADJACENT;
+  t->inverse = inverse;
+  t->pos = rope_pos;
+  t->pos_stride = rope_pos_stride;
+  for (int32_t f = 0; f < t->half; ++f) {
+    const float w = rope->inv_freq[f];
+    if (!(w >= -1024.f && w <= 1024.f))
+      return fail(CONDUIT_ERR_INVALID_ARG, "inv_freq[%d] = %g is not finite or above 1024 in magnitude", f, w);
+    const int32_t a = rope->axis ? rope->axis[f] : 0;
+    if (a < 0 || a >= rope->n_axes)
+      return fail(CONDUIT_ERR_INVALID_ARG, "axis[%d] = %d outside [0, %d)", f, a, rope->n_axes);
+    t->inv_freq[f] = w;
+    t->axis[f] = (uint8_t)a;
+  }
+  return CONDUIT_OK;
+}
+
+// A tensor of dense rows: pointer, alignment and row stride.
+conduit_status check_rows(const void *p, int64_t stride, int64_t row, int32_t dtype, const char *what) {
+  if (!p || !aligned16(p)) return fail(CONDUIT_ERR_INVALID_ARG, "%s must be non-NULL and 16-byte aligned", what);
+  if (stride < row)
+    return fail(CONDUIT_ERR_INVALID_ARG, "%s: row stride %lld below a row of %lld elements", what, (long long)stride,
+                (long long)row);
+  if (stride >= kMaxStrideBytes / esize(dtype))
+    return fail(CONDUIT_ERR_UNSUPPORTED, "%s: row stride of %lld elements (supported: below 32 MiB)", what,
+                (long long)stride);
+  if (stride * esize(dtype) % 16)
+    return fail(CONDUIT_ERR_INVALID_ARG, "%s: row stride must be a multiple of 16 bytes", what);
+  return CONDUIT_OK;
+}
+
+conduit_status check_dtype(int32_t dtype) {
+  if (dtype != CONDUIT_F32 && dtype != CONDUIT_BF16)
+    return fail(CONDUIT_ERR_INVALID_ARG, "dtype %d is not a conduit_dtype", dtype);
+  return CONDUIT_OK;
+}
+
+// The new rows of a cache with these heads, into rp.
+conduit_status check_new_rows(const conduit_rows *rows, const int32_t *pos, int32_t n_q_heads, int32_t n_kv_heads,
+                              int32_t head_dim, RowParams *rp) {
+  if (!pos || reinterpret_cast<uintptr_t>(pos) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "pos must be non-NULL and 4-byte aligned");
+  const int64_t kv_row = (int64_t)n_kv_heads * head_dim, q_row = (int64_t)n_q_heads * head_dim;
+  conduit_status st = check_rows(rows->k, rows->k_stride, kv_row, rows->dtype, "rows->k");
+  if (!st) st = check_rows(rows->v, rows->v_stride, kv_row, rows->dtype, "rows->v");
+  if (!st && !rows->q != !rows->q_out) st = fail(CONDUIT_ERR_INVALID_ARG, "q and q_out go together");
+  if (!st && rows->q) st = check_rows(rows->q, rows->q_stride, q_row, rows->dtype, "rows->q");
+  if (!st && rows->q) st = check_rows(rows->q_out, rows->q_out_stride, q_row, rows->dtype, "rows->q_out");
+  if (!st && rows->q && rows->q == rows->q_out && rows->q_stride != rows->q_out_stride)
+    st = fail(CONDUIT_ERR_INVALID_ARG, "q_out in place of q must have its stride");
+  if (st) return st;
+  rp->n = rows->n;
+  rp->n_q_heads = rows->q ? n_q_heads : 0;
+  rp->n_kv_heads = n_kv_heads;
+  rp->head_dim = head_dim;
+  rp->q = rows->q;
+  rp->q_out = rows->q_out;
+  rp->q_stride = rows->q_stride;
+  rp->q_out_stride = rows->q_out_stride;
+  rp->k_new = rows->k;
+  rp->v_new = rows->v;
+  rp->k_new_stride = rows->k_stride;
+  rp->v_new_stride = rows->v_stride;
+  rp->pos = pos;
+  return CONDUIT_OK;
+}
+
+void cache_params(const conduit_kv *kv, RowParams *rp) {
+  rp->k = kv->k;
+  rp->v = kv->v;
+  rp->k_stride = kv->k_stride;
+  rp->v_stride = kv->v_stride;
+  rp->pages = pages_of(kv);
+  rp->n_ctx = kv->n_ctx;
+}
+
+conduit_status check_mx(const conduit_kv_mx *mx) {
+  if (!mx) return fail(CONDUIT_ERR_INVALID_ARG, "mx is NULL");
+  if (!mx->k || !mx->v || !mx->k_scale || !mx->v_scale)
+    return fail(CONDUIT_ERR_INVALID_ARG, "a pool of mx is NULL");
+  if (!aligned16(mx->k) || !aligned16(mx->v) || !aligned16(mx->k_scale) || !aligned16(mx->v_scale))
+    return fail(CONDUIT_ERR_INVALID_ARG, "the pools of mx must be 16-byte aligned");
+  if (mx->n_kv_heads < 1 || mx->n_q_heads < 1) return fail(CONDUIT_ERR_INVALID_ARG, "head counts must be >= 1");
+  if (mx->n_kv_heads > 256)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "n_kv_heads %d (supported: up to 256)", mx->n_kv_heads);
+  if (mx->n_q_heads % mx->n_kv_heads)
+    return fail(CONDUIT_ERR_INVALID_ARG, "n_q_heads %d is not a multiple of n_kv_heads %d", mx->n_q_heads,
+                mx->n_kv_heads);
+  if (mx->head_dim != 64 && mx->head_dim != 128)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", mx->head_dim);
+  const int32_t ps = mx->page_size;
+  if (ps < 1 || (ps & (ps - 1)) != 0)
+    return fail(CONDUIT_ERR_INVALID_ARG, "page_size %d is not a power of two", ps);
+  if (ps < 64 || ps > (1 << 20))
+    return fail(CONDUIT_ERR_UNSUPPORTED, "page_size %d (supported: powers of two from 64 to 2^20)", ps);
+  if (mx->n_pages < 1 || mx->n_seqs < 1 || mx->table_stride < 1)
+    return fail(CONDUIT_ERR_INVALID_ARG, "n_pages, n_seqs and table_stride must be >= 1");
+  const int64_t page = (int64_t)mx->n_kv_heads * ps;
+  if (mx->code_stride < page * (mx->head_dim / 2) || mx->scale_stride < page * (mx->head_dim / 32))
+    return fail(CONDUIT_ERR_INVALID_ARG, "page strides (%lld, %lld) below a page of %lld codes and %lld scales",
+                (long long)mx->code_stride, (long long)mx->scale_stride, (long long)(page * (mx->head_dim / 2)),
+                (long long)(page * (mx->head_dim / 32)));
+  if (mx->code_stride % 16 || mx->scale_stride % 16)
+    return fail(CONDUIT_ERR_INVALID_ARG, "page strides must be multiples of 16 bytes");
+  if (mx->code_stride > INT64_MAX / mx->n_pages || mx->scale_stride > INT64_MAX / mx->n_pages)
+    return fail(CONDUIT_ERR_INVALID_ARG, "n_pages times a page stride exceeds 64 bits");
+  if (mx->n_ctx < 1 || mx->n_ctx > (int64_t)mx->table_stride * ps)
+    return fail(CONDUIT_ERR_INVALID_ARG, "n_ctx = %d outside [1, table_stride * page_size]", mx->n_ctx);
+  if (mx->n_ctx > (1 << 30)) return fail(CONDUIT_ERR_UNSUPPORTED, "n_ctx = %d (supported: up to 2^30)", mx->n_ctx);
+  if (mx->block_table) {
+    if (reinterpret_cast<uintptr_t>(mx->block_table) % 4)
+      return fail(CONDUIT_ERR_INVALID_ARG, "block_table must be 4-byte aligned");
+  } else if ((int64_t)mx->n_seqs * mx->table_stride > mx->n_pages) {
+    return fail(CONDUIT_ERR_INVALID_ARG, "without a block table n_pages must be at least n_seqs * table_stride");
+  }
+  return CONDUIT_OK;
+}
+
+// n rows shared out over the sequences of a checked descriptor.
+conduit_status mx_cache(const conduit_kv_mx *mx, int32_t n, MxCache *c) {
+  if (n < 0 || n % mx->n_seqs)
+    return fail(CONDUIT_ERR_INVALID_ARG, "n = %d rows are not a multiple of the %d sequences", n, mx->n_seqs);
+  c->k = static_cast<uint8_t *>(mx->k);
+  c->v = static_cast<uint8_t *>(mx->v);
+  c->k_scale = static_cast<uint8_t *>(mx->k_scale);
+  c->v_scale = static_cast<uint8_t *>(mx->v_scale);
+  c->code_stride = mx->code_stride;
+  c->scale_stride = mx->scale_stride;
+  c->table = mx->block_table;
+  c->table_stride = mx->table_stride;
+  c->shift = __builtin_ctz((unsigned)mx->page_size);
+  c->n_pages = mx->n_pages;
+  c->n_ctx = mx->n_ctx;
+  c->n_kv_heads = mx->n_kv_heads;
+  c->rows_per_seq = n / mx->n_seqs;
+  return CONDUIT_OK;
+}
+
+constexpr int64_t kMxMaxPairs = int64_t(1) << 24;
+
+}  // namespace
+
+conduit_status conduit_rotary(const void *x, int64_t x_stride, int32_t n, int32_t n_heads, int32_t head_dim,
+                              int32_t dtype, const conduit_rope *rope, const int32_t *rope_pos,
+                              int64_t rope_pos_stride, int32_t inverse, void *out, int64_t out_stride,
+                              hipStream_t stream) {
+  conduit_status st = check_dtype(dtype);
+  if (st) return st;
+  if (n < 0) return fail(CONDUIT_ERR_INVALID_ARG, "n = %d < 0", n);
+  if (n_heads < 1) return fail(CONDUIT_ERR_INVALID_ARG, "n_heads = %d < 1", n_heads);
+  if (head_dim < 8 || head_dim % 8 || head_dim > CONDUIT_ROTARY_MAX_DIM)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "head_dim %d (supported: multiples of 8 up to %d)", head_dim,
+                CONDUIT_ROTARY_MAX_DIM);
+  if (inverse != 0 && inverse != 1) return fail(CONDUIT_ERR_INVALID_ARG, "inverse must be 0 or 1");
+  if (!rope) return fail(CONDUIT_ERR_INVALID_ARG, "rope is NULL");
+  if (n == 0) return ok();
+  RowParams rp{};
+  const int64_t row = (int64_t)n_heads * head_dim;
+  st = check_rows(x, x_stride, row, dtype, "x");
+  if (!st) st = check_rows(out, out_stride, row, dtype, "out");
+  if (!st && x == out && x_stride != out_stride)
+    st = fail(CONDUIT_ERR_INVALID_ARG, "out in place of x must have its stride");
+  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, head_dim, inverse, 2, &rp.rope);
+  if (st) return st;
+  rp.n = n;
+  rp.n_q_heads = n_heads;
+  rp.head_dim = head_dim;
+  rp.q = x;
+  rp.q_out = out;
+  rp.q_stride = x_stride;
+  rp.q_out_stride = out_stride;
+  const hipError_t e = launch_rows(rp, kRowTurn, dtype == CONDUIT_BF16, stream);
+  if (e != hipSuccess) return hip_fail(e, "rotary");
+  return ok();
+}
+
+conduit_status conduit_append_kv(const conduit_kv *kv, const conduit_rows *rows, const int32_t *pos,
+                                 const conduit_rope *rope, const int32_t *rope_pos, int64_t rope_pos_stride,
+                                 hipStream_t stream) {
+  conduit_status st = check_kv(kv);
+  if (st) return st;
+  if (!rows) return fail(CONDUIT_ERR_INVALID_ARG, "rows is NULL");
+  if (rows->n < 0) return fail(CONDUIT_ERR_INVALID_ARG, "rows->n = %d < 0", rows->n);
+  if (rows->dtype != kv->dtype) return fail(CONDUIT_ERR_INVALID_ARG, "rows->dtype differs from the cache's");
+  if (rows->n == 0) return ok();
+  RowParams rp{};
+  st = check_new_rows(rows, pos, kv->n_q_heads, kv->n_kv_heads, kv->head_dim, &rp);
+  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, rows->n, kv->head_dim, 0, 16, &rp.rope);
+  if (st) return st;
+  cache_params(kv, &rp);
+  const hipError_t e = launch_rows(rp, kRowAppend, kv->dtype == CONDUIT_BF16, stream);
+  if (e != hipSuccess) return hip_fail(e, "append");
+  return ok();
+}
+
+conduit_status conduit_append_mx(const conduit_kv_mx *mx, const conduit_rows *rows, const int32_t *pos,
+                                 const conduit_rope *rope, const int32_t *rope_pos, int64_t rope_pos_stride,
+                                 void *k_out, void *v_out, hipStream_t stream) {
+  conduit_status st = check_mx(mx);
+  if (st) return st;
+  if (!rows) return fail(CONDUIT_ERR_INVALID_ARG, "rows is NULL");
+  st = check_dtype(rows->dtype);
+  RowParams rp{};
+  if (!st) st = mx_cache(mx, rows->n, &rp.mx);
+  if (st) return st;
+  if (rows->n == 0) return ok();
+  st = check_new_rows(rows, pos, mx->n_q_heads, mx->n_kv_heads, mx->head_dim, &rp);
+  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, rows->n, mx->head_dim, 0, 16, &rp.rope);
+  if (!st && ((k_out && !aligned16(k_out)) || (v_out && !aligned16(v_out))))
+    st = fail(CONDUIT_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  if (st) return st;
+  rp.k_out = k_out;
+  rp.v_out = v_out;
+  const hipError_t e = launch_rows(rp, kRowAppendMx, rows->dtype == CONDUIT_BF16, stream);
+  if (e != hipSuccess) return hip_fail(e, "append in 4 bits");
+  return ok();
+}
+
+conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, int32_t n, const conduit_kv *kv,
+                               const int32_t *dst_pos, const conduit_rope *rope, const int32_t *rope_pos,
+                               int64_t rope_pos_stride, hipStream_t stream) {
+  conduit_status st = check_mx(mx);
+  if (!st) st = check_kv(kv);
+  RowParams rp{};
+  if (!st) st = mx_cache(mx, n, &rp.mx);
+  if (st) return st;
+  if (kv->n_kv_heads != mx->n_kv_heads || kv->head_dim != mx->head_dim)
+    return fail(CONDUIT_ERR_INVALID_ARG, "the caches differ in n_kv_heads or head_dim");
+  if (n == 0) return ok();
+  if (!src_pos || !dst_pos || reinterpret_cast<uintptr_t>(src_pos) % 4 || reinterpret_cast<uintptr_t>(dst_pos) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "src_pos and dst_pos must be non-NULL and 4-byte aligned");
+  st = rope_table(rope, rope_pos, rope_pos_stride, n, mx->head_dim, 0, 16, &rp.rope);
+  if (st) return st;
+  rp.n = n;
+  rp.n_kv_heads = mx->n_kv_heads;
+  rp.head_dim = mx->head_dim;
+  rp.pos = dst_pos;
+  rp.src_pos = src_pos;
+  cache_params(kv, &rp);
+  const hipError_t e = launch_rows(rp, kRowLoadMx, kv->dtype == CONDUIT_BF16, stream);
+  if (e != hipSuccess) return hip_fail(e, "load from 4 bits");
+  return ok();
+}
+
+size_t conduit_attn_mx_workspace_bytes(const conduit_kv_mx *mx, int32_t n, int32_t dtype) {
+  if (!mx || n < 1 || mx->n_seqs < 1 || n % mx->n_seqs || mx->n_kv_heads < 1 || mx->n_q_heads < mx->n_kv_heads ||
+      mx->n_ctx < 1 || (mx->head_dim != 64 && mx->head_dim != 128) || (int64_t)n * mx->n_q_heads > kMxMaxPairs)
+    return 0;
+  return mx_attn_shape(mx->n_seqs, n / mx->n_seqs, mx->n_q_heads, mx->n_kv_heads, mx->n_ctx, mx->head_dim,
+                       dtype == CONDUIT_BF16).total;
+}
+
+conduit_status conduit_attn_mx(const conduit_kv_mx *mx, const void *q, int32_t dtype, const int32_t *pos, int32_t n,
+                               float scale, void *o_out, float *lse_out, void *ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  conduit_status st = check_mx(mx);
+  MxAttnParams ap{};
+  if (!st) st = check_dtype(dtype);
+  if (!st) st = mx_cache(mx, n, &ap.mx);
+  if (st) return st;
+  if (!(scale > 0.f) || scale == __builtin_inff()) return fail(CONDUIT_ERR_INVALID_ARG, "scale must be finite and > 0");
+  if ((int64_t)n * mx->n_q_heads > kMxMaxPairs)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "n * n_q_heads = %lld exceeds %lld", (long long)n * mx->n_q_heads,
+                (long long)kMxMaxPairs);
+  if (n == 0) return ok();
+  if (!pos || reinterpret_cast<uintptr_t>(pos) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "pos must be non-NULL and 4-byte aligned");
+  if (!q || !aligned16(q) || !o_out || !aligned16(o_out))
+    return fail(CONDUIT_ERR_INVALID_ARG, "q and o_out must be non-NULL and 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(lse_out) % 4) return fail(CONDUIT_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
+  const bool bf16 = dtype == CONDUIT_BF16;
+  const MxAttnShape sh = mx_attn_shape(mx->n_seqs, ap.mx.rows_per_seq, mx->n_q_heads, mx->n_kv_heads, mx->n_ctx,
+                                       mx->head_dim, bf16);
+  st = check_ws(ws, ws_bytes, sh.total);
+  if (st) return st;
+  ap.n_seqs = mx->n_seqs;
+  ap.n_q_heads = mx->n_q_heads;
+  ap.group = mx->n_q_heads / mx->n_kv_heads;
+  ap.blocks_per_seq = sh.blocks_per_seq;
+  ap.n_workers = sh.n_workers;
+  ap.q = q;
+  ap.pos = pos;
+  ap.scale_log2 = scale * kLog2e;
+  ap.o_out = o_out;
+  ap.lse_out = lse_out;
+  if (sh.total) {
+    ap.prefix = reinterpret_cast<int32_t *>(at(ws, sh.prefix));
+    ap.part_ml = reinterpret_cast<float2 *>(at(ws, sh.ml));
+    ap.part_o = reinterpret_cast<float *>(at(ws, sh.o));
+  }
+  const hipError_t e = launch_attn_mx(ap, sh, mx->head_dim, bf16, stream);
+  if (e != hipSuccess) return hip_fail(e, "attention over 4 bits");
   return ok();
 }
 
