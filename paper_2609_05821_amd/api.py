@@ -499,9 +499,11 @@ def mx_desc(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: to
     _one_device(k, v, k_scale, v_scale, block_table)
     code_stride = k.stride(0) if n_pages > 1 else hkv * page * half
     scale_stride = k_scale.stride(0) if n_pages > 1 else hkv * page * (half // 16)
-    return KVMX(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), code_stride, scale_stride, n_pages,
+    desc = KVMX(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), code_stride, scale_stride, n_pages,
                 page, n_seqs, table_stride, table_stride * page if n_ctx is None else n_ctx, _ptr(block_table),
                 n_q_heads, hkv, 2 * half)
+    desc.tensors = (k, v, k_scale, v_scale, block_table)  # kept alive with the descriptor
+    return desc
 
 
 def _one_device(*tensors) -> Optional[torch.device]:
