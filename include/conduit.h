@@ -446,6 +446,8 @@ conduit_status conduit_residual_error(const conduit_kv *kv, const void *q, int32
  * and then to the tensor's dtype.  A factor on cosine and sine (as some context
  * extensions use) belongs into the attention's scale instead.
  * HOST memory, read during the call only (a captured call keeps what it read).
+ * A call that turns, appends or loads rows takes up to 2^31 - 4096 heads in all
+ * (rows times heads; CONDUIT_ERR_UNSUPPORTED past it).
  * ------------------------------------------------------------------------ */
 #define CONDUIT_MAX_AXES 4
 #define CONDUIT_ROTARY_MAX_DIM 256

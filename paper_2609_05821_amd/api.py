@@ -506,34 +506,50 @@ def mx_desc(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: to
     return desc
 
 
-def _one_device(*tensors) -> Optional[torch.device]:
-    devs = {t.device for t in tensors if t is not None}
-    if len(devs) > 1:
-        raise ConduitError(ERR_INVALID_ARG, f"tensors on different devices: {sorted(map(str, devs))}")
-    return devs.pop() if devs else None
+def _one_device(*tensors) -> int:
+    """Index of the GPU that holds the tensors, -1 for the CPU."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            d = t.get_device()
+            if dev is None:
+                dev = d
+            elif d != dev:
+                raise ConduitError(ERR_INVALID_ARG, f"tensors on different devices (GPU {dev} and {d}; -1: the CPU)")
+    return -1 if dev is None else dev
 
 
 def _call(fn, tensors, stream, *args) -> None:
     """fn(*args, stream) with the tensors' device current: one device for all, the
     current stream of that device unless one is given."""
     dev = _one_device(*tensors)
-    if dev is None or dev.type != "cuda":
+    if dev < 0:
         raise ConduitError(ERR_INVALID_ARG, "tensors must be on the GPU")
-    if stream is not None and stream.device != dev:
-        raise ConduitError(ERR_INVALID_ARG, f"stream of {stream.device} for tensors on {dev}")
-    with torch.cuda.device(dev):
-        _check(fn(*args, (stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream))
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(dev)
+    elif stream.device_index != dev:
+        raise ConduitError(ERR_INVALID_ARG, f"stream of GPU {stream.device_index} for tensors on GPU {dev}")
+    else:
+        raw = stream.cuda_stream
+    if torch._C._cuda_getDevice() == dev:
+        status = fn(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, raw)
+    if status != OK:
+        _check(status)
 
 
 def _heads(t: torch.Tensor, what: str) -> int:
     """Row stride of [n, H, d] with dense heads (any row stride)."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] != 1 and t.stride(1) != t.shape[2]):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or stride[2] != 1 or (shape[1] != 1 and stride[1] != shape[2]):
         raise ConduitError(ERR_INVALID_ARG, f"{what} must be [n, H, d] with dense heads")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _row_ids(t: torch.Tensor, n: int, what: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
         raise ConduitError(ERR_INVALID_ARG, f"{what} must be dense int32 [{n}]")
     return t
 

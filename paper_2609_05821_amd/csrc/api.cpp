@@ -1218,6 +1218,7 @@ conduit_status rope_table(const conduit_rope *rope, const int32_t *rope_pos, int
   if (rope->n_axes > 1 && rope_pos_stride < n)
     return fail(CONDUIT_ERR_INVALID_ARG, "rope_pos_stride %lld below the %d rows", (long long)rope_pos_stride, n);
   t->half = rope->rot_dim / 2;
+  t->n_axes = rope->n_axes;
   t->adjacent = rope->pairing == CONDUIT_PAIR_ADJACENT;
   t->inverse = inverse;
   t->pos = rope_pos;
@@ -1232,6 +1233,14 @@ conduit_status rope_table(const conduit_rope *rope, const int32_t *rope_pos, int
     t->inv_freq[f] = w;
     t->axis[f] = (uint8_t)a;
   }
+  return CONDUIT_OK;
+}
+
+// The row kernel numbers all heads of all rows with 31 bits.
+conduit_status check_heads(int32_t n, int64_t heads) {
+  if (n * heads > INT32_MAX - 4095)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "%d rows of %lld heads (supported: up to 2^31 - 4096 heads in all)", n,
+                (long long)heads);
   return CONDUIT_OK;
 }
 
@@ -1266,6 +1275,7 @@ conduit_status check_new_rows(const conduit_rows *rows, const int32_t *pos, int3
   if (!st && !rows->q != !rows->q_out) st = fail(CONDUIT_ERR_INVALID_ARG, "q and q_out go together");
   if (!st && rows->q) st = check_rows(rows->q, rows->q_stride, q_row, rows->dtype, "rows->q");
   if (!st && rows->q) st = check_rows(rows->q_out, rows->q_out_stride, q_row, rows->dtype, "rows->q_out");
+  if (!st) st = check_heads(rows->n, (int64_t)n_kv_heads + (rows->q ? n_q_heads : 0));
   if (!st && rows->q && rows->q == rows->q_out && rows->q_stride != rows->q_out_stride)
     st = fail(CONDUIT_ERR_INVALID_ARG, "q_out in place of q must have its stride");
   if (st) return st;
@@ -1380,6 +1390,7 @@ conduit_status conduit_rotary(const void *x, int64_t x_stride, int32_t n, int32_
   if (!st) st = check_rows(out, out_stride, row, dtype, "out");
   if (!st && x == out && x_stride != out_stride)
     st = fail(CONDUIT_ERR_INVALID_ARG, "out in place of x must have its stride");
+  if (!st) st = check_heads(n, n_heads);
   if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, head_dim, inverse, 2, &rp.rope);
   if (st) return st;
   rp.n = n;
@@ -1449,7 +1460,8 @@ conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, 
   if (n == 0) return ok();
   if (!src_pos || !dst_pos || reinterpret_cast<uintptr_t>(src_pos) % 4 || reinterpret_cast<uintptr_t>(dst_pos) % 4)
     return fail(CONDUIT_ERR_INVALID_ARG, "src_pos and dst_pos must be non-NULL and 4-byte aligned");
-  st = rope_table(rope, rope_pos, rope_pos_stride, n, mx->head_dim, 0, 16, &rp.rope);
+  st = check_heads(n, mx->n_kv_heads);
+  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, mx->head_dim, 0, 16, &rp.rope);
   if (st) return st;
   rp.n = n;
   rp.n_kv_heads = mx->n_kv_heads;

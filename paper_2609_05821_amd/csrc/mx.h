@@ -10,6 +10,7 @@ namespace conduit {
 constexpr int kMaxRotHalf = 128;
 struct RopeTable {
   int32_t half;                 // rot_dim / 2; 0: nothing turns
+  int32_t n_axes;               // up to 4
   int32_t adjacent;             // pairs (2f, 2f + 1) instead of (f, f + half)
   int32_t inverse;
   const int32_t *pos;           // [axes][n]
@@ -54,7 +55,6 @@ enum RowMode {
 
 struct RowParams {
   int32_t n;
-  int32_t rows_per_block;
   int32_t n_q_heads;            // 0 without queries
   int32_t n_kv_heads;           // 0 for kRowTurn
   int32_t head_dim;

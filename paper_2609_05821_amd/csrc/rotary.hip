@@ -1,17 +1,26 @@
 // Rotary positions, appends to caches of 16, 32 and 4 bits, and loads from the
 // 4-bit cache, gfx950.
 //
-// One kernel body serves all of them: a workgroup takes a few consecutive
-// rows.  First its threads compute the rows' sines and cosines, one (row,
-// frequency) each, in 64 bits into LDS; every head of a row then uses them.
-// Then each wave takes heads of these rows, a lane 8 dims of a head (16 bytes in
-// bf16): it loads them and their partners in the pairs, turns them, and writes
-// them where they go.  The work is bound by memory (each element read and
-// written once; partners come from L1): about 3 flops per element against 4 or
-// 8 bytes.  64-bit arithmetic is therefore free here (v_fma_f64 issues at the
-// rate of an fp32 one on this chip), and it makes the rounding to 4 bits
-// reproducible: no fp32 error of an angle or a product can move a value over a
-// border between two codes.
+// One kernel body serves all of them.  The heads of all rows are one list; a wave
+// takes one or two times as many as its 64 lanes hold, issues all their loads,
+// works out the angles of the rows that they belong to, a lane per frequency, in
+// 64 bits, into LDS of its own, and turns and writes them.  Waves neither loop
+// nor wait for each other: the work is bound by memory (about 3 flops per
+// element against 4 or 8 bytes), and waves that come and go keep more reads in
+// flight than longer-lived ones that prefetch, because a wave's loads and stores
+// retire in order (65,536 rows of 4 KV heads packed: in a loop over items, which
+// waited for its own stores, 105 us; without the loop 82 us).  Where all of a head
+// turns in halves, a lane holds both dims of its pairs, so that no partner is
+// loaded a second time (72 us), and a head's codes leave in one piece (70 us, 4.4
+// TB/s; a copy of that size reaches 5.2 TB/s).  16,384 rows of 16 heads of 80 in
+// fp32: 34 us, 4.9 TB/s; 17,024 rows of 36 heads of 128 in bf16: 65 us, 4.8 TB/s;
+// 65,536 rows loaded from 4 bits: 38 us, 4.5 TB/s.
+// 64-bit arithmetic fits under the loads (v_fma_f64 issues at the rate of an
+// fp32 one on this chip), and it makes the rounding to 4 bits reproducible: no
+// fp32 error of an angle or a product can move a value over a border between
+// two codes.
+#include <algorithm>
+
 #include "mx.h"
 
 namespace conduit {
@@ -19,6 +28,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVec = 8;  // dims of a lane
+constexpr int kWaves = kThreads / 64;
+// Heads of a wave in units of what its lanes hold, where a row has as many: their
+// angles are shared.  17,024 rows of 36 heads: 1 unit 82 us, 2 units 65 us, 3 units
+// 65 us; with few rows 1 keeps more waves busy.
+constexpr int kMany = 2;
+constexpr int64_t kManyFrom = 8192;  // units of work from which on
+constexpr int kDppShl4 = 0x104;  // lane i <- lane i + 4 of its 16
 typedef double f64x2 __attribute__((ext_vector_type(2)));
 
 // (cos, sin) of a = p * f: a is reduced by the nearest multiple of pi/2 (two-part
@@ -52,72 +68,106 @@ __device__ __forceinline__ f64x2 cos_sin(double a) {
   return f64x2{q == 1 || q == 2 ? -cc : cc, q >= 2 ? -ss : ss};
 }
 
+// 8 elements as loaded, and their values.
 template <typename T>
-struct Elem;
-template <>
-struct Elem<u16> {
-  static __device__ __forceinline__ void load(const u16 *p, float (&x)[kVec]) {
-    const u32x4 r = ld16(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __builtin_bit_cast(float, r[j] << 16);
-      x[2 * j + 1] = __builtin_bit_cast(float, r[j] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ float one(const u16 *p) { return bf16_to_f32(*p); }
-  static __device__ __forceinline__ void store(u16 *p, const float (&x)[kVec]) {
-    u32x4 r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bf16x2 b = {static_cast<__bf16>(x[2 * j]), static_cast<__bf16>(x[2 * j + 1])};
-      r[j] = __builtin_bit_cast(uint32_t, b);
-    }
-    st16(p, r);
-  }
-  static __device__ __forceinline__ float rounded(float x) { return bf16_to_f32(f32_to_bf16(x)); }
+struct Raw {
+  u32x4 w[sizeof(T) / 2];
 };
-template <>
-struct Elem<float> {
-  static __device__ __forceinline__ void load(const float *p, float (&x)[kVec]) {
-    const f32x4 a = __builtin_bit_cast(f32x4, ld16(p)), b = __builtin_bit_cast(f32x4, ld16(p + 4));
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T *p) {
+  Raw<T> r;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ld16(p + 8 * i / (sizeof(T) / 2));
+  return r;
+}
+__device__ __forceinline__ void expand(const Raw<u16> &r, float (&x)[kVec]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = __builtin_bit_cast(float, r.w[0][j] << 16);
+    x[2 * j + 1] = __builtin_bit_cast(float, r.w[0][j] & 0xffff0000u);
   }
-  static __device__ __forceinline__ float one(const float *p) { return *p; }
-  static __device__ __forceinline__ void store(float *p, const float (&x)[kVec]) {
-    st16(p, __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}));
-    st16(p + 4, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
+}
+__device__ __forceinline__ void expand(const Raw<float> &r, float (&x)[kVec]) {
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) {
+    const uint32_t w = r.w[j / 4][j % 4];  // (a copy: a bit cast of the vector's element itself reads element 0)
+    x[j] = __builtin_bit_cast(float, w);
   }
-  static __device__ __forceinline__ float rounded(float x) { return x; }
-};
+}
+// What is written here is read by another kernel, if at all soon by other XCDs:
+// streaming stores keep it out of the L2's way (65,536 rows loaded from 4 bits:
+// 51 us against 64 us with ordinary stores).
+__device__ __forceinline__ void st16_stream(void *p, u32x4 v) {
+  __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
+}
+template <typename T>
+__device__ __forceinline__ void store_raw(T *p, const Raw<T> &r) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) st16_stream(p + 8 * i / (sizeof(T) / 2), r.w[i]);
+}
+__device__ __forceinline__ void store(u16 *p, const float (&x)[kVec]) {
+  u32x4 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bf16x2 b = {static_cast<__bf16>(x[2 * j]), static_cast<__bf16>(x[2 * j + 1])};
+    r[j] = __builtin_bit_cast(uint32_t, b);
+  }
+  st16_stream(p, r);
+}
+__device__ __forceinline__ void store(float *p, const float (&x)[kVec]) {
+  st16_stream(p, __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}));
+  st16_stream(p + 4, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
+}
+__device__ __forceinline__ float rounded(float x, u16) { return bf16_to_f32(f32_to_bf16(x)); }
+__device__ __forceinline__ float rounded(float x, float) { return x; }
+__device__ __forceinline__ float one(const u16 *p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ float one(const float *p) { return *p; }
 
-// Dims [o, o + 8) of a head turned in place: x holds them, partner(i) gives dims
-// [i, i + 8) of the same head, cs the row's cosines and sines.
-template <class Partner>
-__device__ __forceinline__ void turn(float (&x)[kVec], int o, int half, bool adjacent, const f64x2 *cs,
-                                     Partner &&partner) {
+// A result in fp32, kept as such: the compiler must not merge this rounding with
+// the one to bf16 that follows (two roundings and one differ near ties).
+__device__ __forceinline__ float to_f32(double x) {
+  float r = (float)x;
+  asm("" : "+v"(r));
+  return r;
+}
+
+// The turn, in place.  x[0] holds dims [o, o + 8) of a head, cs the row's cosines
+// and sines.  FULL: x[1] holds their partners, dims [o + half, o + half + 8).
+// Otherwise y holds the partners (halves; dims from 2 half on have none), or the
+// pairs lie side by side in x[0] (adjacent).
+template <bool FULL, int NV>
+__device__ __forceinline__ void turn(float (&x)[NV][kVec], const float (&y)[kVec], int o, int half, bool adjacent,
+                                     const f64x2 *cs) {
+  if constexpr (FULL) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const f64x2 t = cs[o + j];
+      const double a = x[0][j], b = x[1][j];
+      x[0][j] = to_f32(__builtin_fma(a, t[0], -(b * t[1])));
+      x[1][j] = to_f32(__builtin_fma(b, t[0], a * t[1]));
+    }
+    return;
+  }
   if (o >= 2 * half) return;
   if (adjacent) {
 #pragma unroll
     for (int j = 0; j < kVec / 2; ++j) {
       if (o / 2 + j < half) {
         const f64x2 t = cs[o / 2 + j];
-        const double a = x[2 * j], b = x[2 * j + 1];
-        x[2 * j] = (float)__builtin_fma(a, t[0], -(b * t[1]));
-        x[2 * j + 1] = (float)__builtin_fma(a, t[1], b * t[0]);
+        const double a = x[0][2 * j], b = x[0][2 * j + 1];
+        x[0][2 * j] = to_f32(__builtin_fma(a, t[0], -(b * t[1])));
+        x[0][2 * j + 1] = to_f32(__builtin_fma(b, t[0], a * t[1]));
       }
     }
     return;
   }
   const bool first = o < half;
-  const int f = first ? o : o - half;
-  float y[kVec];
-  partner(first ? o + half : o - half, y);
+  const f64x2 *f = cs + (first ? o : o - half);
 #pragma unroll
   for (int j = 0; j < kVec; ++j) {
-    const f64x2 t = cs[f + j];
+    const f64x2 t = f[j];
     const double m = (double)y[j] * t[1];
-    x[j] = (float)__builtin_fma((double)x[j], t[0], first ? -m : m);
+    x[0][j] = to_f32(__builtin_fma((double)x[0][j], t[0], first ? -m : m));
   }
 }
 
@@ -130,8 +180,8 @@ __device__ __forceinline__ void turn_single(float (&x)[kVec], int o, int half, c
     if (i >= 2 * half) continue;
     const bool first = i < half;
     const f64x2 t = cs[first ? i : i - half];
-    const double m = (double)Elem<T>::one(head + (first ? i + half : i - half)) * t[1];
-    x[j] = (float)__builtin_fma((double)x[j], t[0], first ? -m : m);
+    const double m = (double)one(head + (first ? i + half : i - half)) * t[1];
+    x[j] = to_f32(__builtin_fma((double)x[j], t[0], first ? -m : m));
   }
 }
 
@@ -176,157 +226,295 @@ __device__ __forceinline__ bool any_not_finite(const float (&x)[kVec]) {
   return m >= 0x7f800000u;
 }
 
-// SINGLE: halves whose length is not a multiple of 8 (kRowTurn only).
-// Work unit of a lane group: one query head, or one KV head's keys and values.
-// A group is head_dim / 8 lanes and never straddles two waves, so that a call
-// in place reads every partner before it writes (loads of a wave precede its
-// stores).
-template <typename T, RowMode MODE, bool SINGLE>
-__global__ __launch_bounds__(kThreads) void rows_kernel(RowParams p) {
-  extern __shared__ f64x2 s_cs[];  // [rows of the block][half]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int half = p.rope.half;
-  const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
-  const int rows = (int)min((int64_t)p.rows_per_block, p.n - row0);
-  for (int e = tid; e < rows * half; e += kThreads) {
-    const int r = e / half, f = e - r * half;
-    const int at = p.rope.pos[p.rope.axis[f] * p.rope.pos_stride + row0 + r];
-    f64x2 t = cos_sin((double)at * (double)p.rope.inv_freq[f]);
-    if (p.rope.inverse) t[1] = -t[1];
-    s_cs[e] = t;
-  }
-  __syncthreads();
+// How a head is shared out over lanes.
+enum HeadShape {
+  kVectors = 0,  // 8 dims a lane, partners loaded as well where there are any
+  kPairs = 1,    // all of the head turns, halves: 8 dims of each half a lane
+  kSingles = 2   // 8 dims a lane, partners one by one: halves that 8 does not divide (kRowTurn only)
+};
 
-  const int D = p.head_dim, lanes = D / kVec;      // lanes of a head
-  const int heads = 64 / lanes;                    // heads of a wave
+// A head's lanes are lanes of one wave, so a call in place reads every partner
+// before it writes (loads of a wave precede its stores).
+template <typename T, RowMode MODE, int K, HeadShape SHAPE>
+__global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParams p) {
+  constexpr bool kToKv = MODE == kRowAppend || MODE == kRowLoadMx, kMx = MODE == kRowAppendMx || MODE == kRowLoadMx;
+  constexpr bool kFull = SHAPE == kPairs;
+  constexpr int NV = kFull ? 2 : 1;  // vectors of 8 dims of a lane
+  // K = 1: at most 64 / lanes rows of 4 * NV * lanes frequencies each; K > 1 (a
+  // row has that many heads and more): two rows of up to 128.
+  __shared__ f64x2 s_cs[kWaves][256 * NV];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = p.rope.half, D = p.head_dim;
+  const int lanes = D / (kVec * NV), heads = 64 / lanes;  // lanes of a head, heads of the wave's lanes
   const int sub = lane / lanes, o = (lane - sub * lanes) * kVec;
-  const int units = p.n_q_heads + p.n_kv_heads;    // of a row
+  const int units = p.n_q_heads + p.n_kv_heads;           // query heads, then KV heads, of a row
+  const int total = p.n * units;
   const bool adjacent = p.rope.adjacent != 0;
-  if (sub >= heads) return;
-  for (int u = wave * heads + sub; u < rows * units; u += kThreads / 64 * heads) {
-    const int r = u / units, unit = u - r * units;
-    const int64_t row = row0 + r;
-    const f64x2 *cs = s_cs + r * half;
-    float x[kVec];
-    if (unit < p.n_q_heads) {
-      const T *src = static_cast<const T *>(p.q) + row * p.q_stride + unit * D;
-      Elem<T>::load(src + o, x);
-      if constexpr (SINGLE)
-        turn_single<T>(x, o, half, cs, src);
-      else
-        turn(x, o, half, adjacent, cs, [&](int i, float (&y)[kVec]) { Elem<T>::load(src + i, y); });
-      Elem<T>::store(static_cast<T *>(p.q_out) + row * p.q_out_stride + unit * D + o, x);
-      continue;
-    }
-    if constexpr (MODE == kRowTurn) continue;
-    const int h = unit - p.n_q_heads;
-    if constexpr (MODE == kRowAppend) {
-      const int at = p.pos[row];
-      if ((uint32_t)at >= (uint32_t)p.n_ctx) continue;
-      const int64_t dst = kv_row(p.pages, at);
-      const T *src = static_cast<const T *>(p.k_new) + row * p.k_new_stride + h * D;
-      const T *vs = static_cast<const T *>(p.v_new) + row * p.v_new_stride + h * D + o;
-      T *vd = static_cast<T *>(p.v) + dst * p.v_stride + h * D + o;
-      const u32x4 va = ld16(vs);
-      if constexpr (sizeof(T) == 4) st16(vd + 4, ld16(vs + 4));
-      Elem<T>::load(src + o, x);
-      turn(x, o, half, adjacent, cs, [&](int i, float (&y)[kVec]) { Elem<T>::load(src + i, y); });
-      Elem<T>::store(static_cast<T *>(p.k) + dst * p.k_stride + h * D + o, x);
-      st16(vd, va);
-    }
-    if constexpr (MODE == kRowAppendMx) {
-      const T *src = static_cast<const T *>(p.k_new) + row * p.k_new_stride + h * D;
-      float v[kVec];
-      Elem<T>::load(static_cast<const T *>(p.v_new) + row * p.v_new_stride + h * D + o, v);
-      Elem<T>::load(src + o, x);
-      const bool bad = any_not_finite(x) || any_not_finite(v);
-      turn(x, o, half, adjacent, cs, [&](int i, float (&y)[kVec]) { Elem<T>::load(src + i, y); });
+  const bool partners = SHAPE == kVectors && !adjacent && half > 0;
+  const int partner = o < half ? o + half : o < 2 * half ? o - half : o;
+  auto dims = [&](int i) __attribute__((always_inline)) { return o + i * half; };  // first dim of vector i
+  f64x2 *cs = s_cs[wave];
+  const int first = (blockIdx.x * kWaves + wave) * (heads * K);  // heads of this wave: [first, first + heads * K)
+  if (first >= total) return;
+  const int row0 = first / units, row1 = (min(first + heads * K, total) - 1) / units;
+
+  struct In {
+    int32_t row, unit;         // of the lane
+    int32_t at, from, page, mx_page;
+    bool live;
+    Raw<T> x[NV], y, v[NV];
+    uint32_t xc[NV], yc, vc[NV];  // 4-bit rows
+    int32_t xs[NV], ys, vs[NV];
+  };
+  In in[K];
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[j] = Elem<T>::rounded(x[j]);
-      int ks = block_scale(x), vsc = block_scale(v);
-      uint32_t kc = pack(x, ks), vc = pack(v, vsc);
-      // a head with an infinity or a NaN among its keys or values (before or
-      // after the turn): the key is NaN, the value 0
-      const uint64_t bads = __ballot(bad || any_not_finite(x));
-      if (bads >> (sub * lanes) & (lanes == 16 ? 0xffffull : 0xffull)) {
-        ks = kMxScaleNan;
-        vsc = kMxScaleMin;
-        kc = vc = 0;
+  for (int k = 0; k < K; ++k) {
+    In &c = in[k];
+    const int u = min(first + k * heads + min(sub, heads - 1), total - 1);  // (past the end: loads the last head)
+    c.row = u / units;
+    c.unit = u - c.row * units;
+    if constexpr (MODE != kRowTurn) {
+      c.at = c.from = p.pos[c.row];
+      if constexpr (MODE == kRowLoadMx) c.from = p.src_pos[c.row];
+    }
+    if constexpr (MODE != kRowLoadMx) {
+      const bool query = MODE == kRowTurn || c.unit < p.n_q_heads;
+      const int h = query ? c.unit : c.unit - p.n_q_heads;
+      const T *src =
+          static_cast<const T *>(query ? p.q : p.k_new) + c.row * (query ? p.q_stride : p.k_new_stride) + h * D;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) c.x[i] = load_raw<T>(src + dims(i));
+      c.y = c.x[0];
+      if (partners) c.y = load_raw<T>(src + partner);
+      if constexpr (MODE != kRowTurn) {
+        const T *vsrc = static_cast<const T *>(p.v_new) + c.row * p.v_new_stride + h * D;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          c.v[i] = c.x[i];
+          if (!query) c.v[i] = load_raw<T>(vsrc + dims(i));
+        }
       }
-      if (p.k_out) {
-        float y[kVec];
-        unpack(kc, ks, y);
-        Elem<T>::store(static_cast<T *>(p.k_out) + (row * p.n_kv_heads + h) * D + o, y);
-      }
-      if (p.v_out) {
-        float y[kVec];
-        unpack(vc, vsc, y);
-        Elem<T>::store(static_cast<T *>(p.v_out) + (row * p.n_kv_heads + h) * D + o, y);
-      }
-      const int at = p.pos[row];
-      if ((uint32_t)at >= (uint32_t)p.mx.n_ctx) continue;
-      const int64_t page = mx_page(p.mx, (int)(row / p.mx.rows_per_seq), at);
-      const int64_t slot = ((int64_t)h << p.mx.shift) + (at & ((1 << p.mx.shift) - 1));  // of the page
-      const int64_t co = page * p.mx.code_stride + slot * (D / 2) + o / 2;
-      const int64_t so = page * p.mx.scale_stride + slot * (D / kMxBlock) + o / kMxBlock;
-      *reinterpret_cast<uint32_t *>(p.mx.k + co) = kc;
-      *reinterpret_cast<uint32_t *>(p.mx.v + co) = vc;
-      if (o % kMxBlock == 0) {
-        p.mx.k_scale[so] = (uint8_t)ks;
-        p.mx.v_scale[so] = (uint8_t)vsc;
-      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    In &c = in[k];
+    if constexpr (MODE != kRowTurn) {
+      c.live = true;
+      if constexpr (kToKv) c.live = c.live && (uint32_t)c.at < (uint32_t)p.n_ctx;
+      if constexpr (kMx) c.live = c.live && (uint32_t)c.from < (uint32_t)p.mx.n_ctx;
+      if (!c.live) c.at = c.from = 0;  // (a row that is left out: token 0, not written)
+      if constexpr (kToKv)
+        if (p.pages.table) c.page = p.pages.table[c.at >> p.pages.shift];
+      if constexpr (kMx) c.mx_page = mx_page(p.mx, c.row / p.mx.rows_per_seq, c.from);
     }
     if constexpr (MODE == kRowLoadMx) {
-      const int from = p.src_pos[row], at = p.pos[row];
-      if ((uint32_t)from >= (uint32_t)p.mx.n_ctx || (uint32_t)at >= (uint32_t)p.n_ctx) continue;
-      const int64_t page = mx_page(p.mx, (int)(row / p.mx.rows_per_seq), from);
-      const int64_t slot = ((int64_t)h << p.mx.shift) + (from & ((1 << p.mx.shift) - 1));
-      const int64_t co = page * p.mx.code_stride + slot * (D / 2);
-      const int64_t so = page * p.mx.scale_stride + slot * (D / kMxBlock);
-      auto key = [&](int i, float (&y)[kVec]) {
-        unpack(*reinterpret_cast<const uint32_t *>(p.mx.k + co + i / 2), p.mx.k_scale[so + i / kMxBlock], y);
-      };
-      float v[kVec];
-      unpack(*reinterpret_cast<const uint32_t *>(p.mx.v + co + o / 2), p.mx.v_scale[so + o / kMxBlock], v);
-      key(o, x);
-      turn(x, o, half, adjacent, cs, key);
-      const int64_t dst = kv_row(p.pages, at);
-      Elem<T>::store(static_cast<T *>(p.k) + dst * p.k_stride + h * D + o, x);
-      Elem<T>::store(static_cast<T *>(p.v) + dst * p.v_stride + h * D + o, v);
+      const int64_t slot = ((int64_t)c.unit << p.mx.shift) + (c.from & ((1 << p.mx.shift) - 1));
+      const int64_t co = c.mx_page * p.mx.code_stride + slot * (D / 2);
+      const int64_t so = c.mx_page * p.mx.scale_stride + slot * (D / kMxBlock);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        c.xc[i] = *reinterpret_cast<const uint32_t *>(p.mx.k + co + dims(i) / 2);
+        c.vc[i] = *reinterpret_cast<const uint32_t *>(p.mx.v + co + dims(i) / 2);
+        c.xs[i] = p.mx.k_scale[so + dims(i) / kMxBlock];
+        c.vs[i] = p.mx.v_scale[so + dims(i) / kMxBlock];
+      }
+      c.yc = c.xc[0];
+      c.ys = c.xs[0];
+      if (partners) {
+        c.yc = *reinterpret_cast<const uint32_t *>(p.mx.k + co + partner / 2);
+        c.ys = p.mx.k_scale[so + partner / kMxBlock];
+      }
+    }
+  }
+  // The rows' angles.
+  const int n_angles = (row1 - row0 + 1) * half;
+  for (int e = lane; e < n_angles; e += 64) {
+    const int r = e / half, f = e - r * half;
+    // (the positions on all axes, so that none waits for the frequency's axis)
+    const int32_t *pos = p.rope.pos + row0 + r;
+    int32_t at[4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) at[a] = a < p.rope.n_axes ? pos[a * p.rope.pos_stride] : 0;
+    const int axis = p.rope.axis[f];
+    f64x2 t = cos_sin((double)(axis < 2 ? axis ? at[1] : at[0] : axis == 2 ? at[2] : at[3]) *
+                      (double)p.rope.inv_freq[f]);
+    if (p.rope.inverse) t[1] = -t[1];
+    cs[e] = t;
+  }
+  // (this wave's LDS accesses stay in order in the hardware)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const In &c = in[k];
+    if (sub >= heads || first + k * heads + sub >= total) return;
+    const f64x2 *rcs = cs + (c.row - row0) * half;
+    float x[NV][kVec], y[kVec], v[NV][kVec];
+    if constexpr (MODE == kRowLoadMx) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        unpack(c.xc[i], c.xs[i], x[i]);
+        unpack(c.vc[i], c.vs[i], v[i]);
+      }
+      unpack(c.yc, c.ys, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) expand(c.x[i], x[i]);
+      expand(c.y, y);
+    }
+    bool bad = false;  // an infinity or a NaN
+    if constexpr (MODE == kRowAppendMx) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) bad = bad || any_not_finite(x[i]);
+    }
+    if constexpr (SHAPE == kSingles)
+      turn_single<T>(x[0], o, half, rcs, static_cast<const T *>(p.q) + c.row * p.q_stride + c.unit * D);
+    else
+      turn<kFull>(x, y, o, half, adjacent, rcs);
+    if (MODE == kRowTurn || c.unit < p.n_q_heads) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        store(static_cast<T *>(p.q_out) + c.row * p.q_out_stride + c.unit * D + dims(i), x[i]);
+      continue;
+    }
+    const int h = c.unit - p.n_q_heads;
+    if constexpr (kToKv) {
+      if (!c.live) continue;
+      int64_t row = c.at;
+      if (p.pages.table)
+        row = ((int64_t)min(max(c.page, 0), p.pages.n_pages - 1) << p.pages.shift) |
+              (c.at & ((1 << p.pages.shift) - 1));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        store(static_cast<T *>(p.k) + row * p.k_stride + h * D + dims(i), x[i]);
+        T *vd = static_cast<T *>(p.v) + row * p.v_stride + h * D + dims(i);
+        if constexpr (MODE == kRowAppend)
+          store_raw(vd, c.v[i]);
+        else
+          store(vd, v[i]);
+      }
+    }
+    if constexpr (MODE == kRowAppendMx) {
+      int ks[NV], vs[NV];
+      uint32_t kc[NV], vc[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        expand(c.v[i], v[i]);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[i][j] = rounded(x[i][j], T{});
+        ks[i] = block_scale(x[i]);
+        vs[i] = block_scale(v[i]);
+        kc[i] = pack(x[i], ks[i]);
+        vc[i] = pack(v[i], vs[i]);
+        bad = bad || any_not_finite(x[i]) || any_not_finite(v[i]);
+      }
+      // a head with an infinity or a NaN among its keys or values, before or
+      // after the turn: the key is NaN, the value 0
+      if (__ballot(bad) >> (sub * lanes) & ((1ull << lanes) - 1)) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          ks[i] = kMxScaleNan;
+          vs[i] = kMxScaleMin;
+          kc[i] = vc[i] = 0;
+        }
+      }
+      const int64_t held = ((int64_t)c.row * p.n_kv_heads + h) * D;
+      const int64_t slot = ((int64_t)h << p.mx.shift) + (c.from & ((1 << p.mx.shift) - 1));  // of the page
+      const int64_t co = c.mx_page * p.mx.code_stride + slot * (D / 2);
+      const int64_t so = c.mx_page * p.mx.scale_stride + slot * (D / kMxBlock);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int d = dims(i);
+        if (p.k_out) {
+          unpack(kc[i], ks[i], y);
+          store(static_cast<T *>(p.k_out) + held + d, y);
+        }
+        if (p.v_out) {
+          unpack(vc[i], vs[i], y);
+          store(static_cast<T *>(p.v_out) + held + d, y);
+        }
+      }
+      if (!c.live) continue;
+      if constexpr (kFull) {
+        // Neighbouring lanes swap a dword, so that a lane writes 8 bytes and a
+        // head's codes go out in one piece; its scales are put together in its
+        // first lane.
+        const bool odd = o & kVec;
+        const int64_t at = co + (odd ? half + o - kVec : o) / 2;
+        auto codes = [&](uint8_t *pool, const uint32_t (&x)[NV]) __attribute__((always_inline)) {
+          const uint32_t other = dpp_mov<kDppXor1>(0u, odd ? x[0] : x[1]);
+          *reinterpret_cast<uint2 *>(pool + at) = odd ? make_uint2(other, x[1]) : make_uint2(x[0], other);
+        };
+        auto scales = [&](uint8_t *pool, const int (&x)[NV]) __attribute__((always_inline)) {
+          if (lanes == 8) {  // blocks 0 and 2 in the first quad, 1 and 3 in the second
+            const uint32_t mine = x[0] | x[1] << 16, next = dpp_mov<kDppShl4>(0u, mine);
+            if (o == 0) *reinterpret_cast<uint32_t *>(pool + so) = mine | next << 8;
+          } else if (o == 0) {
+            *reinterpret_cast<uint16_t *>(pool + so) = (uint16_t)(x[0] | x[1] << 8);
+          }
+        };
+        codes(p.mx.k, kc);
+        codes(p.mx.v, vc);
+        scales(p.mx.k_scale, ks);
+        scales(p.mx.v_scale, vs);
+      } else {
+        *reinterpret_cast<uint32_t *>(p.mx.k + co + o / 2) = kc[0];
+        *reinterpret_cast<uint32_t *>(p.mx.v + co + o / 2) = vc[0];
+        if (o % kMxBlock == 0) {
+          p.mx.k_scale[so + o / kMxBlock] = (uint8_t)ks[0];
+          p.mx.v_scale[so + o / kMxBlock] = (uint8_t)vs[0];
+        }
+      }
     }
   }
 }
 
-template <typename T>
-void launch_mode(const RowParams &p, RowMode mode, dim3 grid, size_t lds, hipStream_t s) {
-  if (mode == kRowTurn && !p.rope.adjacent && p.rope.half % kVec)
-    rows_kernel<T, kRowTurn, true><<<grid, kThreads, lds, s>>>(p);
-  else if (mode == kRowTurn)
-    rows_kernel<T, kRowTurn, false><<<grid, kThreads, lds, s>>>(p);
-  else if (mode == kRowAppend)
-    rows_kernel<T, kRowAppend, false><<<grid, kThreads, lds, s>>>(p);
-  else if (mode == kRowAppendMx)
-    rows_kernel<T, kRowAppendMx, false><<<grid, kThreads, lds, s>>>(p);
+template <typename T, int K, HeadShape SHAPE>
+void launch_mode(const RowParams &p, RowMode mode, dim3 grid, hipStream_t s) {
+  if (mode == kRowTurn)
+    rows_kernel<T, kRowTurn, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
+  else if constexpr (SHAPE != kSingles) {
+    if (mode == kRowAppend)
+      rows_kernel<T, kRowAppend, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
+    else if (mode == kRowAppendMx)
+      rows_kernel<T, kRowAppendMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
+    else
+      rows_kernel<T, kRowLoadMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
+  }
+}
+
+template <typename T, int K>
+void launch_shape(const RowParams &p, RowMode mode, HeadShape shape, dim3 grid, hipStream_t s) {
+  if (shape == kPairs)
+    launch_mode<T, K, kPairs>(p, mode, grid, s);
+  else if (shape == kVectors)
+    launch_mode<T, K, kVectors>(p, mode, grid, s);
   else
-    rows_kernel<T, kRowLoadMx, false><<<grid, kThreads, lds, s>>>(p);
+    launch_mode<T, K, kSingles>(p, mode, grid, s);
 }
 
 }  // namespace
 
-hipError_t launch_rows(const RowParams &p_in, RowMode mode, bool bf16, hipStream_t s) {
+hipError_t launch_rows(const RowParams &p, RowMode mode, bool bf16, hipStream_t s) {
   static const char *const names[] = {"rotary", "append", "append_mx", "load_mx"};
   ProfScope ps(names[mode], s);
-  RowParams p = p_in;
-  // Rows of a workgroup: up to 8 share one pass over the angles' code and keep
-  // its LDS at 16 KB or less; fewer while there are not enough workgroups for
-  // every CU to hold several.
-  p.rows_per_block = (int32_t)min(8, max(1, p.n / 1024));
-  const dim3 grid((p.n + p.rows_per_block - 1) / p.rows_per_block);
-  const size_t lds = (size_t)p.rows_per_block * p.rope.half * sizeof(f64x2);
+  const int half = p.rope.half;
+  const HeadShape shape = p.rope.adjacent || !half ? kVectors
+                          : half % kVec           ? kSingles
+                          : 2 * half == p.head_dim ? kPairs
+                                                   : kVectors;
+  const int heads = 64 / (p.head_dim / (kVec * (shape == kPairs ? 2 : 1))), units = p.n_q_heads + p.n_kv_heads;
+  const int64_t total = (int64_t)p.n * units;
+  const bool many = units >= kMany * heads && total >= kManyFrom * heads;
+  const int k = many ? kMany : 1;
+  const dim3 grid((unsigned)((total + heads * k * kWaves - 1) / (heads * k * kWaves)));
   if (bf16)
-    launch_mode<u16>(p, mode, grid, lds, s);
+    many ? launch_shape<u16, kMany>(p, mode, shape, grid, s) : launch_shape<u16, 1>(p, mode, shape, grid, s);
   else
-    launch_mode<float>(p, mode, grid, lds, s);
+    many ? launch_shape<float, kMany>(p, mode, shape, grid, s) : launch_shape<float, 1>(p, mode, shape, grid, s);
   return hipGetLastError();
 }
 

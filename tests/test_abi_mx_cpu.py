@@ -67,7 +67,8 @@ def rotary(x=FAKE, xs=3584, n=5, heads=28, d=128, dtype=api.BF16, r=None, pos=FA
     (dict(r=rope(rot_dim=130)), INV), (dict(r=rope(rot_dim=63)), INV), (dict(r=rope(rot_dim=0)), INV),
     (dict(r=rope(n_axes=0)), INV), (dict(r=rope(n_axes=5)), INV), (dict(r=rope(pairing=2)), INV),
     (dict(r=rope(axes=2), ps=4), INV), (dict(r=rope(freq=float("nan"))), INV), (dict(r=rope(freq=float("inf"))), INV),
-    (dict(r=rope(freq=1025.0)), INV), (dict(r=rope(axes=2, axis=[2] * 64)), INV),
+    (dict(r=rope(freq=1025.0)), INV), (dict(n=(1 << 31) - 1, heads=1, xs=128, os_=128, ps=1 << 31), UNS),
+    (dict(n=76700000, ps=1 << 31), UNS), (dict(r=rope(axes=2, axis=[2] * 64)), INV),
     (dict(r=rope(axes=2, axis=[-1] * 64)), INV), (dict(r=rope(inv_freq=None)), INV)])
 def test_rotary_rejects(case, status):
     assert rotary(**case) == status
@@ -83,7 +84,7 @@ def append(k=None, r=None, pos=FAKE, ro=None, rp=FAKE, ps=3):
 ROW_CASES = [
     (dict(k=0), INV), (dict(v=FAKE + 8), INV), (dict(k_stride=508), INV), (dict(v_stride=516), INV),
     (dict(k_stride=1 << 24), UNS), (dict(n=-3), INV), (dict(q_out=0), INV), (dict(q=0), INV), (dict(q=FAKE + 2), INV),
-    (dict(q_stride=3580), INV), (dict(q_out_stride=3585), INV), (dict(q_out_stride=3592), INV)]
+    (dict(n=(1 << 31) - 1), UNS), (dict(n=67200000), UNS), (dict(q_stride=3580), INV), (dict(q_out_stride=3585), INV), (dict(q_out_stride=3592), INV)]
 
 
 @pytest.mark.parametrize("case,status", ROW_CASES + [(dict(dtype=api.F32), INV)])
@@ -149,6 +150,7 @@ def test_append_mx_and_load_reject():
     assert L.conduit_load_mx(b(m), 0, 3, b(k), FAKE, None, None, 0, None) == INV
     assert L.conduit_load_mx(b(m), FAKE, 3, b(k), FAKE + 1, None, None, 0, None) == INV
     assert L.conduit_load_mx(b(m), FAKE, 3, b(k), FAKE, b(ro.desc), None, 3, None) == INV
+    assert L.conduit_load_mx(b(m), FAKE, 1 << 29, b(k), FAKE, None, None, 0, None) == UNS
     other = kv(n_kv_heads=2)
     assert L.conduit_load_mx(b(m), FAKE, 3, b(other), FAKE, None, None, 0, None) == INV
     other = kv(head_dim=64)
