@@ -27,6 +27,10 @@
 namespace conduit {
 namespace {
 
+#ifndef THICK_OCC
+#define THICK_OCC 2
+#define THICK_MT 2
+#endif
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kMInit = -1e30f;  // initial running maximum (log2 units)
 // The running maximum moves when a step exceeds it by more than this many log2
@@ -92,19 +96,78 @@ __device__ __forceinline__ int wave_min_i(int x) {
 // Keys 0 .. n - 1 that a row at position `pos` may see, n <= n_ctx.
 __device__ __forceinline__ int keys_seen(int pos, int n_ctx) { return min(max(pos, -1), n_ctx - 1) + 1; }
 
-// Key steps of sequence block sb for one KV head.
-__device__ __forceinline__ int block_steps(const MxAttnParams &p, int sb, int pairs) {
+// Steps of `step` keys of sequence block sb for one KV head (positions loaded
+// eight at a time).
+__device__ __forceinline__ int block_steps(const MxAttnParams &p, int sb, int pairs, int step) {
   const int s = sb / p.blocks_per_seq, rb = sb - s * p.blocks_per_seq, r = p.mx.rows_per_seq;
   const int lo = rb * pairs / p.group, hi = min((rb * pairs + pairs - 1) / p.group, r - 1);
-  int n = 0;
-  for (int i = lo; i <= hi; ++i) n = max(n, keys_seen(p.pos[(int64_t)s * r + i], p.mx.n_ctx));
-  return (n + kStep - 1) / kStep;
+  const int32_t *pos = p.pos + (int64_t)s * r;
+  int top = -1;
+  for (int i = lo; i <= hi; i += 8) {
+    int x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = pos[min(i + j, hi)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, x[j]);
+  }
+  return (keys_seen(top, p.mx.n_ctx) + step - 1) / step;
 }
 
 // Workgroups that share `total` steps: no fewer than kMinSteps each.
 constexpr int kMinSteps = 2;
 __device__ __forceinline__ int workers(int n_workers, int total) { return min(n_workers, max(1, total / kMinSteps)); }
 __device__ __forceinline__ int part_begin(int w, int total, int n) { return (int)((int64_t)w * total / n); }
+
+// The list of key steps of the whole call (prefix: steps before each sequence
+// block, block by block and there KV head by KV head) and the part [t, t_end) of
+// this workgroup.  False: no part.  Workgroup 0 keeps the list for the merge.
+__device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int step, int *s_sum, int *s_prefix,
+                                          int &t, int &t_end) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_sb = p.n_seqs * p.blocks_per_seq;
+  int total = 0;
+  for (int b0 = 0; b0 < n_sb; b0 += kThreads) {
+    const int sb = b0 + tid;
+    const int own = sb < n_sb ? block_steps(p, sb, pairs, step) * p.mx.n_kv_heads : 0;
+    const int incl = (int)wave_inclusive_sum((uint32_t)own);
+    __syncthreads();
+    if (lane == 63) s_sum[wave] = incl;
+    __syncthreads();
+    int before = total;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) before += s_sum[w];
+      total += s_sum[w];
+    }
+    if (sb < n_sb) s_prefix[sb] = before + incl - own;
+  }
+  if (tid == 0) s_prefix[n_sb] = total;
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int i = tid; i <= n_sb; i += kThreads) p.prefix[i] = s_prefix[i];
+  const int n = workers(p.n_workers, total);
+  if ((int)blockIdx.x >= n) return false;
+  t = __builtin_amdgcn_readfirstlane(part_begin(blockIdx.x, total, n));
+  t_end = __builtin_amdgcn_readfirstlane(part_begin(blockIdx.x + 1, total, n));
+  return true;
+}
+
+// What of a part that begins at step t lies in one (sequence block, KV head):
+// its steps [first, last) of `steps`.
+struct Segment {
+  int sb, h, first, last, steps;
+};
+__device__ __forceinline__ Segment segment_at(const MxAttnParams &p, int n_sb, const int *s_prefix, int t, int t_end) {
+  int lo = 0, hi = n_sb - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (s_prefix[mid + 1] > t) hi = mid;
+    else lo = mid + 1;
+  }
+  const int begin = s_prefix[lo], steps = (s_prefix[lo + 1] - begin) / p.mx.n_kv_heads;
+  const int h = (t - begin) / steps, first = t - begin - h * steps;
+  return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(h), __builtin_amdgcn_readfirstlane(first),
+          __builtin_amdgcn_readfirstlane(min(steps, first + t_end - t)), __builtin_amdgcn_readfirstlane(steps)};
+}
 
 // One 32-key step of a wave in registers.
 template <int D>
@@ -117,8 +180,7 @@ struct Step {
 };
 
 template <int D>
-__device__ __forceinline__ void load_step(const MxCache &c, int seq, int h, int key0, int lane, Step<D> &st) {
-  const int64_t page = mx_page(c, seq, key0);
+__device__ __forceinline__ void load_step(const MxCache &c, int64_t page, int h, int key0, int lane, Step<D> &st) {
   const int64_t slot = ((int64_t)h << c.shift) + (key0 & ((1 << c.shift) - 1));
   const uint8_t *k = c.k + page * c.code_stride + slot * (D / 2);
   const uint8_t *v = c.v + page * c.code_stride + slot * (D / 2);
@@ -146,10 +208,15 @@ __device__ __forceinline__ void load_step(const MxCache &c, int seq, int h, int 
   }
 }
 
+// Waves a SIMD holds (workgroups a CU holds) of each variant, by its registers.
+constexpr int waves_per_simd(int D, int MT, int NS) {
+  return D == 128 ? (MT == 1 && NS == 1 ? 3 : MT == 2 && NS == 3 ? 1 : 2) : (MT == 1 ? 3 : 2);
+}
+
 // MT: groups of 16 pairs of a block.  NS: exact bf16 parts of queries and
 // probabilities (1: bf16 tensors, 3: fp32).
 template <int D, int MT, int NS>
-__global__ __launch_bounds__(kThreads) void attn_mx_kernel(MxAttnParams p) {
+__global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_kernel(MxAttnParams p) {
   constexpr int kPairs = 16 * MT;
   constexpr int C = D / 32;            // MFMA steps over the dims
   constexpr int DT = D / 16;           // 16-dim tiles of O^T
@@ -170,57 +237,15 @@ __global__ __launch_bounds__(kThreads) void attn_mx_kernel(MxAttnParams p) {
   float *tile_o = reinterpret_cast<float *>(s_tile[wave]);
 
   // This workgroup's part [t, t_end) of the step list, or block blockIdx.x.
-  int t = 0, t_end = 1, part0 = 0;
-  if (p.n_workers) {
-    int total = 0;
-    for (int b0 = 0; b0 < n_sb; b0 += kThreads) {
-      const int sb = b0 + tid;
-      const int own = sb < n_sb ? block_steps(p, sb, kPairs) * hkv : 0;
-      const int incl = (int)wave_inclusive_sum((uint32_t)own);
-      __syncthreads();
-      if (lane == 63) s_sum[wave] = incl;
-      __syncthreads();
-      int before = total;
-      for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += s_sum[w];
-        total += s_sum[w];
-      }
-      if (sb < n_sb) s_prefix[sb] = before + incl - own;
-    }
-    if (tid == 0) s_prefix[n_sb] = total;
-    __syncthreads();
-    if (blockIdx.x == 0)
-      for (int i = tid; i <= n_sb; i += kThreads) p.prefix[i] = s_prefix[i];
-    const int n = workers(p.n_workers, total);
-    if ((int)blockIdx.x >= n) return;
-    t = part0 = part_begin(blockIdx.x, total, n);
-    t_end = part_begin(blockIdx.x + 1, total, n);
-  }
+  int t = 0, t_end = 1;
+  if (p.n_workers && !plan_part(p, kPairs, kStep, s_sum, s_prefix, t, t_end)) return;
+  const int part0 = t;
 
   while (t < t_end) {
-    int sb, h, first, last, steps = 0;  // block, and its steps [first, last) of this segment
-    if (p.n_workers) {
-      int lo = 0, hi = n_sb - 1;        // the block that holds step t
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (s_prefix[mid + 1] > t) hi = mid;
-        else lo = mid + 1;
-      }
-      sb = __builtin_amdgcn_readfirstlane(lo);
-      steps = (s_prefix[sb + 1] - s_prefix[sb]) / hkv;
-      h = (t - s_prefix[sb]) / steps;
-      first = t - s_prefix[sb] - h * steps;
-      last = min(steps, first + t_end - t);
-      h = __builtin_amdgcn_readfirstlane(h);
-      first = __builtin_amdgcn_readfirstlane(first);
-      last = __builtin_amdgcn_readfirstlane(last);
-      steps = __builtin_amdgcn_readfirstlane(steps);
-    } else {
-      sb = blockIdx.x / hkv;
-      h = blockIdx.x - sb * hkv;
-      first = 0;
-      last = INT32_MAX;
-    }
+    const Segment sg = p.n_workers ? segment_at(p, n_sb, s_prefix, t, t_end)
+                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0};
+    const int sb = sg.sb, h = sg.h, first = sg.first;
+    int last = sg.last;
     const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
     const int n_pairs = min(kPairs, r * G - rb * kPairs);
     const int64_t row_base = (int64_t)seq * r;
@@ -355,25 +380,32 @@ __global__ __launch_bounds__(kThreads) void attn_mx_kernel(MxAttnParams p) {
     };
 
     // Two register sets take turns, so that a step is loaded while the one
-    // before it is used.
+    // before it is used; its page is looked up one step earlier still.
     {
       Step<D> a, b;
       int key0 = first * kStep + wave * kWaveKeys;
       const int end = min(most, last * kStep);  // (last * kStep < n_ctx + kStep <= 2^30 + kStep)
-      if (key0 < end) load_step<D>(p.mx, seq, h, key0, lane, a);
+      auto page_at = [&](int key) __attribute__((always_inline)) { return mx_page(p.mx, seq, min(key, end - 1)); };
+      int page = 0;
+      if (key0 < end) {
+        page = page_at(key0 + kStep);
+        load_step<D>(p.mx, page_at(key0), h, key0, lane, a);
+      }
       while (key0 < end) {
-        if (key0 + kStep < end) load_step<D>(p.mx, seq, h, key0 + kStep, lane, b);
+        if (key0 + kStep < end) load_step<D>(p.mx, page, h, key0 + kStep, lane, b);
+        page = page_at(key0 + 2 * kStep);
         use(a, key0);
         key0 += kStep;
         if (key0 >= end) break;
-        if (key0 + kStep < end) load_step<D>(p.mx, seq, h, key0 + kStep, lane, a);
+        if (key0 + kStep < end) load_step<D>(p.mx, page, h, key0 + kStep, lane, a);
+        page = page_at(key0 + 2 * kStep);
         use(b, key0);
         key0 += kStep;
       }
     }
 
     // The four waves' results, 16 pairs at a time.
-    const bool whole = !p.n_workers || (first == 0 && last == steps);
+    const bool whole = !p.n_workers || (first == 0 && last == sg.steps);
     const int slot = 2 * blockIdx.x + (t == part0 ? 0 : 1);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -429,6 +461,235 @@ __global__ __launch_bounds__(kThreads) void attn_mx_kernel(MxAttnParams p) {
     __syncthreads();  // the tiles are free again
     if (!p.n_workers) break;
     t += last - first;
+  }
+}
+
+// Many pairs per KV head (the selected rows of a refresh): bound by the matrix
+// products and the exponentials between them.  The waves of a workgroup take 16 *
+// MT pairs each and go over the same keys: keys are unpacked by every wave for
+// itself straight into operands (a quarter of a wave's vector work at 32 pairs; through
+// LDS they would cost more of its bandwidth than there is), values once per
+// workgroup into LDS, one 64-key tile ahead.
+constexpr int kTileKeys = 64;
+template <int D, int MT>
+__global__ __launch_bounds__(kThreads, THICK_OCC) void attn_mx_many_kernel(MxAttnParams p) {
+  constexpr int kPairs = 16 * MT * kWaves;
+  constexpr int C = D / 32, DT = D / 16, KW = D / 32;
+  constexpr int VP = D + 16;
+  constexpr int LPK = D / 32;                        // lanes of a key's values
+  constexpr int VK = kTileKeys / kWaves;             // keys whose values a wave unpacks
+  __shared__ __attribute__((aligned(16))) u16 s_v[2][kTileKeys * VP];
+  __shared__ int s_sum[kWaves];
+  extern __shared__ int s_prefix[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  const int hkv = p.mx.n_kv_heads, r = p.mx.rows_per_seq, G = p.group;
+  const int n_sb = p.n_seqs * p.blocks_per_seq;
+  int t = 0, t_end = 1;
+  if (p.n_workers && !plan_part(p, kPairs, kTileKeys, s_sum, s_prefix, t, t_end)) return;
+  const int part0 = t;
+  const MxCache &c = p.mx;
+
+  while (t < t_end) {
+    const Segment sg = p.n_workers ? segment_at(p, n_sb, s_prefix, t, t_end)
+                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0};
+    const int seq = sg.sb / p.blocks_per_seq, rb = sg.sb - seq * p.blocks_per_seq, h = sg.h;
+    const int block0 = rb * kPairs, n_pairs = min(kPairs, r * G - block0);
+    const int64_t row_base = (int64_t)seq * r;
+
+    bf16x8 q[MT][C];
+    int seen[MT];
+    int most = 0, least = INT32_MAX;                 // of this wave's columns
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int j = 16 * (wave * MT + mt) + col, pair = block0 + j;
+      seen[mt] = INT32_MAX;
+#pragma unroll
+      for (int x = 0; x < C; ++x) q[mt][x] = bf16x8{};
+      if (j < n_pairs) {
+        const int row = pair / G;
+        seen[mt] = keys_seen(p.pos[row_base + row], c.n_ctx);
+        most = max(most, seen[mt]);
+        least = min(least, seen[mt]);
+        const u16 *at = static_cast<const u16 *>(p.q) +
+                        ((row_base + row) * p.n_q_heads + h * G + pair % G) * D + g * (D / 4);
+#pragma unroll
+        for (int x = 0; x < C; ++x) q[mt][x] = as_bf16x8(ld16(at + 8 * x));
+      }
+    }
+    most = __builtin_amdgcn_readfirstlane(wave_max_i(most));
+    least = __builtin_amdgcn_readfirstlane(wave_min_i(least));
+    __syncthreads();
+    if (lane == 0) s_sum[wave] = most;
+    __syncthreads();
+    int block_most = 0;
+    for (int w = 0; w < kWaves; ++w) block_most = max(block_most, s_sum[w]);
+    block_most = __builtin_amdgcn_readfirstlane(block_most);
+    const int last = min(sg.last, (block_most + kTileKeys - 1) / kTileKeys);
+
+    f32x4 o[MT][DT];
+    float m[MT], l[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m[mt] = kMInit;
+      l[mt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[mt][dt] = f32x4{};
+    }
+
+    // A tile's keys in registers (this wave's copy) and its share of the values.
+    struct Tile {
+      uint32_t k[4][KW];
+      int ks[4];
+      u32x4 v;
+      int vs;
+    };
+    auto load = [&](int tile, int page_at, Tile &x) __attribute__((always_inline)) {
+      const int64_t page = page_at, slot = ((int64_t)h << c.shift) + ((tile * kTileKeys) & ((1 << c.shift) - 1));
+      const uint8_t *k = c.k + page * c.code_stride + slot * (D / 2);
+      const uint8_t *v = c.v + page * c.code_stride + slot * (D / 2);
+      const uint8_t *ks = c.k_scale + page * c.scale_stride + slot * (D / kMxBlock);
+      const uint8_t *vs = c.v_scale + page * c.scale_stride + slot * (D / kMxBlock);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint8_t *at = k + (16 * j + col) * (D / 2) + g * (D / 8);
+        if constexpr (D == 128) {
+          const u32x4 y = ld16(at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x.k[j][i] = y[i];
+        } else {
+          const uint2 y = *reinterpret_cast<const uint2 *>(at);
+          x.k[j][0] = y.x;
+          x.k[j][1] = y.y;
+        }
+        x.ks[j] = ks[(16 * j + col) * (D / kMxBlock) + g * (D / 4) / kMxBlock];
+      }
+      // (at head_dim 64 half of the lanes hold the wave's 16 keys)
+      const int vl = min(lane, VK * LPK - 1);
+      x.v = ld16(v + wave * VK * (D / 2) + vl * 16);
+      x.vs = vs[wave * VK * (D / kMxBlock) + vl];
+    };
+    auto put_values = [&](int tile, Tile &x) __attribute__((always_inline)) {
+      if (lane >= VK * LPK) return;
+      const int key = wave * VK + lane / LPK;
+      // keys past every row: their values must not reach the product as NaN or
+      // infinity (their probabilities are 0)
+      const bool hidden = tile * kTileKeys + key >= block_most;
+      const float s = scale_of(hidden ? 127 : x.vs);
+      u16 *dst = s_v[tile & 1] + key * VP + (lane % LPK) * 32;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st16(dst + 8 * i, __builtin_bit_cast(u32x4, unpack8(hidden ? 0 : x.v[i], s)));
+    };
+    auto page_of = [&](int tile) __attribute__((always_inline)) {
+      return mx_page(c, seq, min(tile, last - 1) * kTileKeys);
+    };
+
+    if (sg.first < last) {
+      Tile x;
+      int page = page_of(sg.first + 1);
+      load(sg.first, page_of(sg.first), x);
+      put_values(sg.first, x);
+      __syncthreads();
+      for (int tile = sg.first; tile < last; ++tile) {
+        Tile next = x;
+        if (tile + 1 < last) load(tile + 1, page, next);
+        page = page_of(tile + 2);
+        if (tile * kTileKeys < most) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int key0 = tile * kTileKeys + 32 * half;
+            f32x4 s[MT][2];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) s[mt][0] = s[mt][1] = f32x4{};
+#pragma unroll
+            for (int d = 0; d < C; ++d)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const bf16x8 kop = unpack8(x.k[2 * half + j][d], scale_of(x.ks[2 * half + j]));
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                  s[mt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, q[mt][d], s[mt][j], 0, 0, 0);
+              }
+            bf16x8 pr[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              float y[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[i] = s[mt][i >> 2][i & 3];
+              if (key0 + 32 > least) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  y[i] = key0 + 16 * (i >> 2) + 4 * g + (i & 3) < seen[mt] ? y[i] : kNegInf;
+              }
+              float top = y[0];
+#pragma unroll
+              for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
+              top *= p.scale_log2;  // (the scale is positive)
+              if (__any(top > m[mt] + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float mn = fmaxf(m[mt], top), a = fast_exp2(m[mt] - mn);
+                m[mt] = mn;
+                l[mt] *= a;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= a;
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float e = fast_exp2(__builtin_fmaf(y[i], p.scale_log2, -m[mt]));
+                l[mt] += e;
+                pr[mt][i] = static_cast<__bf16>(e);
+              }
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+              const u16 *at = s_v[tile & 1] + (32 * half + 4 * g + (col >> 2)) * VP + 16 * dt + 4 * (col & 3);
+              const short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at));
+              const short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at + 16 * VP));
+              const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt)
+                o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, pr[mt], o[mt][dt], 0, 0, 0);
+            }
+          }
+        }
+        if (tile + 1 < last) put_values(tile + 1, next);
+        x = next;
+        __syncthreads();
+      }
+    }
+
+    const bool whole = !p.n_workers || (sg.first == 0 && sg.last == sg.steps);
+    const int slot = 2 * blockIdx.x + (t == part0 ? 0 : 1);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float lt = l[mt];
+      lt += __shfl_xor(lt, 16, 64);
+      lt += __shfl_xor(lt, 32, 64);
+      const int j = 16 * (wave * MT + mt) + col, pair = block0 + j;
+      if (j >= n_pairs) continue;
+      const int64_t gp = (row_base + pair / G) * p.n_q_heads + h * G + pair % G;
+      const float inv = lt == 0.f ? 0.f : 1.f / lt;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const int e = 16 * dt + 4 * g;
+        if (whole) {
+          const f32x4 y = o[mt][dt] * inv;
+          *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
+              make_ushort4(f32_to_bf16(y[0]), f32_to_bf16(y[1]), f32_to_bf16(y[2]), f32_to_bf16(y[3]));
+        } else {
+          *reinterpret_cast<f32x4 *>(p.part_o + ((int64_t)slot * kPairs + j) * D + e) = o[mt][dt];
+        }
+      }
+      if (g == 0) {
+        if (!whole)
+          p.part_ml[(int64_t)slot * kPairs + j] = make_float2(m[mt], lt);
+        else if (p.lse_out)
+          p.lse_out[gp] = lt == 0.f ? kNegInf : (m[mt] + __log2f(lt)) * kLn2;
+      }
+    }
+    if (!p.n_workers) break;
+    t += sg.last - sg.first;
   }
 }
 
@@ -490,21 +751,19 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int 
   if (e == 0 && p.lse_out) p.lse_out[gp] = L == 0.f ? kNegInf : (M + __log2f(L)) * kLn2;
 }
 
-template <int D, int MT, int NS>
-void launch_thin(const MxAttnParams &p, const MxAttnShape &sh, hipStream_t s) {
+template <int D>
+void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStream_t s) {
   const int n_sb = p.n_seqs * p.blocks_per_seq;
   const int grid = p.n_workers ? p.n_workers : n_sb * p.mx.n_kv_heads;
   const size_t lds = p.n_workers ? (size_t)(n_sb + 1) * 4 : 0;
-  attn_mx_kernel<D, MT, NS><<<grid, kThreads, lds, s>>>(p);
-}
-
-template <int D>
-void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStream_t s) {
-  const bool wide = sh.pairs > 16;
-  if (bf16)
-    wide ? launch_thin<D, 2, 1>(p, sh, s) : launch_thin<D, 1, 1>(p, sh, s);
+  if (sh.pairs > 32)
+    attn_mx_many_kernel<D, THICK_MT><<<grid, kThreads, lds, s>>>(p);
+  else if (bf16)
+    sh.pairs > 16 ? attn_mx_kernel<D, 2, 1><<<grid, kThreads, lds, s>>>(p)
+                  : attn_mx_kernel<D, 1, 1><<<grid, kThreads, lds, s>>>(p);
   else
-    wide ? launch_thin<D, 2, 3>(p, sh, s) : launch_thin<D, 1, 3>(p, sh, s);
+    sh.pairs > 16 ? attn_mx_kernel<D, 2, 3><<<grid, kThreads, lds, s>>>(p)
+                  : attn_mx_kernel<D, 1, 3><<<grid, kThreads, lds, s>>>(p);
 }
 
 }  // namespace
@@ -513,14 +772,17 @@ MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_head
                           int32_t head_dim, bool bf16) {
   MxAttnShape L{};
   const int64_t pairs = (int64_t)rows_per_seq * (n_q_heads / n_kv_heads);
-  L.pairs = pairs <= 16 ? 16 : 32;
+  const bool many = bf16 && pairs > 32;
+  L.pairs = pairs <= 16 ? 16 : many ? 16 * THICK_MT * kWaves : 32;
   L.blocks_per_seq = (int32_t)((pairs + L.pairs - 1) / L.pairs);
   const int64_t n_sb = (int64_t)n_seqs * L.blocks_per_seq, blocks = n_sb * n_kv_heads;
   const int64_t steps = ((int64_t)n_ctx + kStep - 1) / kStep;
+  const int64_t resident =
+      256 * (many ? THICK_OCC : waves_per_simd(head_dim, L.pairs > 16 ? 2 : 1, bf16 ? 1 : 3));
   // Workgroups share the steps out evenly while their parts can be listed and
   // there are steps to share; otherwise one workgroup takes a block.
-  if (steps > 8 && n_sb <= kMaxSeqBlocks && blocks * steps < INT32_MAX)
-    L.n_workers = (int32_t)std::min<int64_t>(768, std::max<int64_t>(1, blocks * steps / kMinSteps));
+  if (steps > 8 && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX)
+    L.n_workers = (int32_t)std::min<int64_t>(resident, std::max<int64_t>(1, blocks * steps / kMinSteps));
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
   if (L.n_workers) {
