@@ -27,9 +27,8 @@
 namespace conduit {
 namespace {
 
-#ifndef THICK_OCC
-#define THICK_OCC 2
-#define THICK_MT 2
+#ifndef SCHED
+#define SCHED
 #endif
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kMInit = -1e30f;  // initial running maximum (log2 units)
@@ -167,6 +166,34 @@ __device__ __forceinline__ Segment segment_at(const MxAttnParams &p, int n_sb, c
   const int h = (t - begin) / steps, first = t - begin - h * steps;
   return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(h), __builtin_amdgcn_readfirstlane(first),
           __builtin_amdgcn_readfirstlane(min(steps, first + t_end - t)), __builtin_amdgcn_readfirstlane(steps)};
+}
+
+// Pages of one sequence, looked up in two parts: the block-table entry is loaded
+// well before it is made a page number.  (A load whose address is the same in
+// every lane would be made scalar, and waited for, at once: the lane's offset is
+// hidden from the compiler.  That wait, for every load in flight, was 1 us a tile.)
+struct SeqPages {
+  __amdgpu_buffer_rsrc_t table;
+  int first;     // page of token 0 without a table
+  bool listed;
+};
+__device__ __forceinline__ SeqPages seq_pages(const MxCache &c, int seq) {
+  const int64_t first = (int64_t)seq * c.table_stride;
+  SeqPages r;
+  r.listed = c.table != nullptr;
+  r.first = (int)first;
+  // (2^24 pages hold 2^30 tokens; a read past the end returns 0)
+  r.table = buffer_rsrc(r.listed ? c.table + first : nullptr, r.listed ? min(c.table_stride, 1 << 24) * 4 : 0);
+  return r;
+}
+__device__ __forceinline__ int page_entry(const SeqPages &s, int i) {
+  int off = i * 4;
+  asm("" : "+v"(off));
+  return __builtin_amdgcn_raw_buffer_load_b32(s.table, off, 0, 0);
+}
+__device__ __forceinline__ int page_number(const MxCache &c, const SeqPages &s, int i, int entry) {
+  const int page = s.listed ? __builtin_amdgcn_readfirstlane(entry) : s.first + i;
+  return min(max(page, 0), c.n_pages - 1);
 }
 
 // One 32-key step of a wave in registers.
@@ -385,20 +412,26 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
       Step<D> a, b;
       int key0 = first * kStep + wave * kWaveKeys;
       const int end = min(most, last * kStep);  // (last * kStep < n_ctx + kStep <= 2^30 + kStep)
-      auto page_at = [&](int key) __attribute__((always_inline)) { return mx_page(p.mx, seq, min(key, end - 1)); };
-      int page = 0;
+      // page of key `key`, or of the last key
+      auto index = [&](int key) __attribute__((always_inline)) { return min(key, end - 1) >> p.mx.shift; };
+      const SeqPages pages = seq_pages(p.mx, seq);
+      int entry = 0;
       if (key0 < end) {
-        page = page_at(key0 + kStep);
-        load_step<D>(p.mx, page_at(key0), h, key0, lane, a);
+        const int now = page_entry(pages, index(key0));
+        entry = page_entry(pages, index(key0 + kStep));
+        load_step<D>(p.mx, page_number(p.mx, pages, index(key0), now), h, key0, lane, a);
       }
+      auto load_next = [&](Step<D> &st) __attribute__((always_inline)) {
+        if (key0 + kStep < end)
+          load_step<D>(p.mx, page_number(p.mx, pages, index(key0 + kStep), entry), h, key0 + kStep, lane, st);
+        entry = page_entry(pages, index(key0 + 2 * kStep));
+      };
       while (key0 < end) {
-        if (key0 + kStep < end) load_step<D>(p.mx, page, h, key0 + kStep, lane, b);
-        page = page_at(key0 + 2 * kStep);
+        load_next(b);
         use(a, key0);
         key0 += kStep;
         if (key0 >= end) break;
-        if (key0 + kStep < end) load_step<D>(p.mx, page, h, key0 + kStep, lane, a);
-        page = page_at(key0 + 2 * kStep);
+        load_next(a);
         use(b, key0);
         key0 += kStep;
       }
@@ -465,16 +498,22 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
 }
 
 // Many pairs per KV head (the selected rows of a refresh): bound by the matrix
-// products and the exponentials between them.  The waves of a workgroup take 16 *
-// MT pairs each and go over the same keys: keys are unpacked by every wave for
-// itself straight into operands (a quarter of a wave's vector work at 32 pairs; through
-// LDS they would cost more of its bandwidth than there is), values once per
-// workgroup into LDS, one 64-key tile ahead.
+// products and the vector work between them.  The waves of a workgroup take 32
+// pairs each and go over the same keys, 64 at a time.  Keys are unpacked by every
+// wave for itself straight into operands, values once per workgroup into LDS, one
+// tile ahead.  Products are v_mfma_f32_32x32x16_bf16: beside it a wave issues
+// vector instructions for free, beside 16x16x32 it does not (16 of the former with
+// 64 fma between them 543 cycles, 32 of the latter, the same products, 659).
+//   S^T: lane (key, h) holds half h of the key's dims, codes and scales in one piece
+//   each; a pair's column is in two lanes, 16 keys each.
+//   O^T: the probabilities are operands as they lie; the values' rows are stored
+//   interleaved (v_interleaved_key) so that the transposing reads hit every bank once.
 constexpr int kTileKeys = 64;
-template <int D, int MT>
-__global__ __launch_bounds__(kThreads, THICK_OCC) void attn_mx_many_kernel(MxAttnParams p) {
-  constexpr int kPairs = 16 * MT * kWaves;
-  constexpr int C = D / 32, DT = D / 16, KW = D / 32;
+constexpr int kManyPairs = 32 * kWaves;
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams p) {
+  constexpr int kPairs = kManyPairs;
+  constexpr int C = D / 16, DT = D / 32;
   constexpr int VP = D + 16;
   constexpr int LPK = D / 32;                        // lanes of a key's values
   constexpr int VK = kTileKeys / kWaves;             // keys whose values a wave unpacks
@@ -482,13 +521,14 @@ __global__ __launch_bounds__(kThreads, THICK_OCC) void attn_mx_many_kernel(MxAtt
   __shared__ int s_sum[kWaves];
   extern __shared__ int s_prefix[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 15, g = lane >> 4;
+  const int col = lane & 31, hh = lane >> 5;
   const int hkv = p.mx.n_kv_heads, r = p.mx.rows_per_seq, G = p.group;
   const int n_sb = p.n_seqs * p.blocks_per_seq;
   int t = 0, t_end = 1;
   if (p.n_workers && !plan_part(p, kPairs, kTileKeys, s_sum, s_prefix, t, t_end)) return;
   const int part0 = t;
   const MxCache &c = p.mx;
+  const int v_lane = v_operand_lane_offset_il<VP>(lane);
 
   while (t < t_end) {
     const Segment sg = p.n_workers ? segment_at(p, n_sb, s_prefix, t, t_end)
@@ -497,28 +537,23 @@ __global__ __launch_bounds__(kThreads, THICK_OCC) void attn_mx_many_kernel(MxAtt
     const int block0 = rb * kPairs, n_pairs = min(kPairs, r * G - block0);
     const int64_t row_base = (int64_t)seq * r;
 
-    bf16x8 q[MT][C];
-    int seen[MT];
-    int most = 0, least = INT32_MAX;                 // of this wave's columns
+    // The lane's pair: its query and how many keys it sees (a lane without one sees
+    // all, so that nothing is masked for it).
+    const int j = 32 * wave + col, pair = block0 + j;
+    bf16x8 q[C];
+    int seen = INT32_MAX, most = 0;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int j = 16 * (wave * MT + mt) + col, pair = block0 + j;
-      seen[mt] = INT32_MAX;
+    for (int x = 0; x < C; ++x) q[x] = bf16x8{};
+    if (j < n_pairs) {
+      const int row = pair / G;
+      seen = most = keys_seen(p.pos[row_base + row], c.n_ctx);
+      const u16 *at = static_cast<const u16 *>(p.q) +
+                      ((row_base + row) * p.n_q_heads + h * G + pair % G) * D + hh * (D / 2);
 #pragma unroll
-      for (int x = 0; x < C; ++x) q[mt][x] = bf16x8{};
-      if (j < n_pairs) {
-        const int row = pair / G;
-        seen[mt] = keys_seen(p.pos[row_base + row], c.n_ctx);
-        most = max(most, seen[mt]);
-        least = min(least, seen[mt]);
-        const u16 *at = static_cast<const u16 *>(p.q) +
-                        ((row_base + row) * p.n_q_heads + h * G + pair % G) * D + g * (D / 4);
-#pragma unroll
-        for (int x = 0; x < C; ++x) q[mt][x] = as_bf16x8(ld16(at + 8 * x));
-      }
+      for (int x = 0; x < C; ++x) q[x] = as_bf16x8(ld16(at + 8 * x));
     }
     most = __builtin_amdgcn_readfirstlane(wave_max_i(most));
-    least = __builtin_amdgcn_readfirstlane(wave_min_i(least));
+    const int least = __builtin_amdgcn_readfirstlane(wave_min_i(seen));
     __syncthreads();
     if (lane == 0) s_sum[wave] = most;
     __syncthreads();
@@ -527,165 +562,172 @@ __global__ __launch_bounds__(kThreads, THICK_OCC) void attn_mx_many_kernel(MxAtt
     block_most = __builtin_amdgcn_readfirstlane(block_most);
     const int last = min(sg.last, (block_most + kTileKeys - 1) / kTileKeys);
 
-    f32x4 o[MT][DT];
-    float m[MT], l[MT];
+    f32x16 o[DT];
+    float m = kMInit, l = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      m[mt] = kMInit;
-      l[mt] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[mt][dt] = f32x4{};
-    }
+    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x16{};
 
-    // A tile's keys in registers (this wave's copy) and its share of the values.
-    struct Tile {
-      uint32_t k[4][KW];
-      int ks[4];
+    // 32 keys in registers (this wave's copy), and its share of a tile's values.
+    struct Keys {
+      uint32_t k[C];
+      uint32_t ks;   // the scale bytes of the lane's dims
+    };
+    struct Values {
       u32x4 v;
       int vs;
     };
-    auto load = [&](int tile, int page_at, Tile &x) __attribute__((always_inline)) {
-      const int64_t page = page_at, slot = ((int64_t)h << c.shift) + ((tile * kTileKeys) & ((1 << c.shift) - 1));
-      const uint8_t *k = c.k + page * c.code_stride + slot * (D / 2);
-      const uint8_t *v = c.v + page * c.code_stride + slot * (D / 2);
-      const uint8_t *ks = c.k_scale + page * c.scale_stride + slot * (D / kMxBlock);
-      const uint8_t *vs = c.v_scale + page * c.scale_stride + slot * (D / kMxBlock);
+    auto slot_of = [&](int tile) __attribute__((always_inline)) {
+      return ((int64_t)h << c.shift) + ((min(tile, last - 1) * kTileKeys) & ((1 << c.shift) - 1));
+    };
+    auto load_keys = [&](int tile, int page, int half, Keys &x) __attribute__((always_inline)) {
+      const int64_t slot = slot_of(tile) + 32 * half;
+      const uint8_t *k = c.k + page * c.code_stride + slot * (D / 2) + col * (D / 2) + hh * (D / 4);
+      const uint8_t *ks = c.k_scale + page * c.scale_stride + slot * (D / kMxBlock) + col * (D / kMxBlock) +
+                          hh * (D / 2 / kMxBlock);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint8_t *at = k + (16 * j + col) * (D / 2) + g * (D / 8);
-        if constexpr (D == 128) {
-          const u32x4 y = ld16(at);
+      for (int i = 0; i < C / 4; ++i) {
+        const u32x4 y = ld16(k + 16 * i);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x.k[j][i] = y[i];
-        } else {
-          const uint2 y = *reinterpret_cast<const uint2 *>(at);
-          x.k[j][0] = y.x;
-          x.k[j][1] = y.y;
-        }
-        x.ks[j] = ks[(16 * j + col) * (D / kMxBlock) + g * (D / 4) / kMxBlock];
+        for (int e = 0; e < 4; ++e) x.k[4 * i + e] = y[e];
       }
+      if constexpr (D == 128)
+        x.ks = *reinterpret_cast<const uint16_t *>(ks);
+      else
+        x.ks = *ks;
+    };
+    auto load_values = [&](int tile, int page, Values &x) __attribute__((always_inline)) {
+      const int64_t slot = slot_of(tile) + wave * VK;
       // (at head_dim 64 half of the lanes hold the wave's 16 keys)
       const int vl = min(lane, VK * LPK - 1);
-      x.v = ld16(v + wave * VK * (D / 2) + vl * 16);
-      x.vs = vs[wave * VK * (D / kMxBlock) + vl];
+      x.v = ld16(c.v + page * c.code_stride + slot * (D / 2) + vl * 16);
+      x.vs = c.v_scale[page * c.scale_stride + slot * (D / kMxBlock) + vl];
     };
-    auto put_values = [&](int tile, Tile &x) __attribute__((always_inline)) {
+    auto put_values = [&](int tile, Values &x) __attribute__((always_inline)) {
       if (lane >= VK * LPK) return;
-      const int key = wave * VK + lane / LPK;
+      const int k16 = lane / LPK;                    // of the wave's 16 keys
       // keys past every row: their values must not reach the product as NaN or
       // infinity (their probabilities are 0)
-      const bool hidden = tile * kTileKeys + key >= block_most;
+      const bool hidden = tile * kTileKeys + wave * VK + k16 >= block_most;
       const float s = scale_of(hidden ? 127 : x.vs);
-      u16 *dst = s_v[tile & 1] + key * VP + (lane % LPK) * 32;
+      const int row = 8 * ((k16 >> 2) & 1) + 2 * (k16 & 3) + (k16 >> 3);
+      u16 *dst = s_v[tile & 1] + (wave * VK + row) * VP + (lane % LPK) * 32;
 #pragma unroll
       for (int i = 0; i < 4; ++i) st16(dst + 8 * i, __builtin_bit_cast(u32x4, unpack8(hidden ? 0 : x.v[i], s)));
     };
-    auto page_of = [&](int tile) __attribute__((always_inline)) {
-      return mx_page(c, seq, min(tile, last - 1) * kTileKeys);
+    const SeqPages pages = seq_pages(c, seq);
+    auto index = [&](int tile) __attribute__((always_inline)) { return min(tile, last - 1) * kTileKeys >> c.shift; };
+    auto page_of = [&](int tile, int entry) __attribute__((always_inline)) {
+      return page_number(c, pages, index(tile), entry);
+    };
+    auto key_operand = [&](const Keys &x, int d) __attribute__((always_inline)) {
+      return unpack8(x.k[d], scale_of(d < 4 ? x.ks & 0xff : x.ks >> 8));
+    };
+    // Softmax and O^T products of 32 keys whose S^T is in s, with the S^T products
+    // of the next 32 (nx) between them, so that matrix and vector work of one
+    // wave overlap.
+    auto half_step = [&](int tile, int half, f32x16 &s, const Keys &nx) __attribute__((always_inline)) {
+      const int key0 = tile * kTileKeys + 32 * half;
+      if (key0 + 32 > least) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = key0 + (i & 3) + 8 * (i >> 2) + 4 * hh < seen ? s[i] : kNegInf;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      top *= p.scale_log2;  // (the scale is positive)
+      if (__any(top > m + kSlack)) {
+        const float mn = fmaxf(m, half_max(top)), a = fast_exp2(m - mn);
+        m = mn;
+        l *= a;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= a;
+      }
+      f32x16 sn{};
+#pragma unroll
+      for (int d = 0; d < C; ++d) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(nx, d), q[d], sn, 0, 0, 0);
+      bf16x8 pr[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = fast_exp2(__builtin_fmaf(s[i], p.scale_log2, -m));
+        l += e;
+        pr[i >> 3][i & 7] = static_cast<__bf16>(e);
+      }
+      const u16 *at = s_v[tile & 1] + 32 * half * VP + v_lane;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand_il<VP>(at + 16 * kk * VP + 32 * dt), pr[kk], o[dt],
+                                                          0, 0, 0);
+      SCHED
+      s = sn;
+    };
+    // A tile: S^T of its first half is in s, its second half's keys are in b, the
+    // next tile's in c0 and d (loaded two half steps before their use).
+    int page1 = 0, entry2 = 0;  // the next tile's page, the table entry of the one after
+    auto tile_step = [&](int tile, f32x16 &s, Keys &a, Keys &b, Keys &c0, Keys &d) __attribute__((always_inline)) {
+      Values v;
+      load_values(tile + 1, page1, v);
+      load_keys(tile + 1, page1, 1, d);
+      const int entry3 = page_entry(pages, index(tile + 3));
+      const bool active = tile * kTileKeys < most;
+      if (active) half_step(tile, 0, s, b);
+      page1 = page_of(tile + 2, entry2);
+      entry2 = entry3;
+      load_keys(tile + 2, page1, 0, a);
+      if (active) half_step(tile, 1, s, c0);
+      if (tile + 1 < last) put_values(tile + 1, v);
+      __syncthreads();
     };
 
     if (sg.first < last) {
-      Tile x;
-      int page = page_of(sg.first + 1);
-      load(sg.first, page_of(sg.first), x);
-      put_values(sg.first, x);
+      Keys k0, k1, k2, k3;
+      f32x16 s{};
+      {
+        const int entry0 = page_entry(pages, index(sg.first)), entry1 = page_entry(pages, index(sg.first + 1));
+        entry2 = page_entry(pages, index(sg.first + 2));
+        const int page = page_of(sg.first, entry0);
+        Values v;
+        load_values(sg.first, page, v);
+        load_keys(sg.first, page, 0, k0);
+        load_keys(sg.first, page, 1, k1);
+        page1 = page_of(sg.first + 1, entry1);
+        load_keys(sg.first + 1, page1, 0, k2);
+        put_values(sg.first, v);
+#pragma unroll
+        for (int d = 0; d < C; ++d) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(k0, d), q[d], s, 0, 0, 0);
+      }
       __syncthreads();
-      for (int tile = sg.first; tile < last; ++tile) {
-        Tile next = x;
-        if (tile + 1 < last) load(tile + 1, page, next);
-        page = page_of(tile + 2);
-        if (tile * kTileKeys < most) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int key0 = tile * kTileKeys + 32 * half;
-            f32x4 s[MT][2];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) s[mt][0] = s[mt][1] = f32x4{};
-#pragma unroll
-            for (int d = 0; d < C; ++d)
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const bf16x8 kop = unpack8(x.k[2 * half + j][d], scale_of(x.ks[2 * half + j]));
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                  s[mt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, q[mt][d], s[mt][j], 0, 0, 0);
-              }
-            bf16x8 pr[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              float y[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) y[i] = s[mt][i >> 2][i & 3];
-              if (key0 + 32 > least) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  y[i] = key0 + 16 * (i >> 2) + 4 * g + (i & 3) < seen[mt] ? y[i] : kNegInf;
-              }
-              float top = y[0];
-#pragma unroll
-              for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
-              top *= p.scale_log2;  // (the scale is positive)
-              if (__any(top > m[mt] + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float mn = fmaxf(m[mt], top), a = fast_exp2(m[mt] - mn);
-                m[mt] = mn;
-                l[mt] *= a;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= a;
-              }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float e = fast_exp2(__builtin_fmaf(y[i], p.scale_log2, -m[mt]));
-                l[mt] += e;
-                pr[mt][i] = static_cast<__bf16>(e);
-              }
-            }
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              const u16 *at = s_v[tile & 1] + (32 * half + 4 * g + (col >> 2)) * VP + 16 * dt + 4 * (col & 3);
-              const short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at));
-              const short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at + 16 * VP));
-              const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt)
-                o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, pr[mt], o[mt][dt], 0, 0, 0);
-            }
-          }
-        }
-        if (tile + 1 < last) put_values(tile + 1, next);
-        x = next;
-        __syncthreads();
+      for (int tile = sg.first; tile < last; tile += 2) {
+        tile_step(tile, s, k0, k1, k2, k3);
+        if (tile + 1 < last) tile_step(tile + 1, s, k2, k3, k0, k1);
       }
     }
 
     const bool whole = !p.n_workers || (sg.first == 0 && sg.last == sg.steps);
     const int slot = 2 * blockIdx.x + (t == part0 ? 0 : 1);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      float lt = l[mt];
-      lt += __shfl_xor(lt, 16, 64);
-      lt += __shfl_xor(lt, 32, 64);
-      const int j = 16 * (wave * MT + mt) + col, pair = block0 + j;
-      if (j >= n_pairs) continue;
+    l += __shfl_xor(l, 32, 64);
+    if (j < n_pairs) {
       const int64_t gp = (row_base + pair / G) * p.n_q_heads + h * G + pair % G;
-      const float inv = lt == 0.f ? 0.f : 1.f / lt;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const int e = 16 * dt + 4 * g;
-        if (whole) {
-          const f32x4 y = o[mt][dt] * inv;
-          *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
-              make_ushort4(f32_to_bf16(y[0]), f32_to_bf16(y[1]), f32_to_bf16(y[2]), f32_to_bf16(y[3]));
-        } else {
-          *reinterpret_cast<f32x4 *>(p.part_o + ((int64_t)slot * kPairs + j) * D + e) = o[mt][dt];
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 32 * dt + 8 * i + 4 * hh;
+          const f32x4 y = {o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+          if (whole)
+            *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
+                make_ushort4(f32_to_bf16(y[0] * inv), f32_to_bf16(y[1] * inv), f32_to_bf16(y[2] * inv),
+                             f32_to_bf16(y[3] * inv));
+          else
+            *reinterpret_cast<f32x4 *>(p.part_o + ((int64_t)slot * kPairs + j) * D + e) = y;
         }
-      }
-      if (g == 0) {
+      if (hh == 0) {
         if (!whole)
-          p.part_ml[(int64_t)slot * kPairs + j] = make_float2(m[mt], lt);
+          p.part_ml[(int64_t)slot * kPairs + j] = make_float2(m, l);
         else if (p.lse_out)
-          p.lse_out[gp] = lt == 0.f ? kNegInf : (m[mt] + __log2f(lt)) * kLn2;
+          p.lse_out[gp] = l == 0.f ? kNegInf : (m + __log2f(l)) * kLn2;
       }
     }
     if (!p.n_workers) break;
@@ -694,57 +736,65 @@ __global__ __launch_bounds__(kThreads, THICK_OCC) void attn_mx_many_kernel(MxAtt
 }
 
 // Merge of the blocks that more than one workgroup worked on, and the outputs
-// of blocks without keys: one workgroup per (row, head) pair, groups of lanes
-// taking turns at the parts.
-template <int D, bool BF16>
+// of blocks without keys.  A workgroup takes PW pairs of a block, a group of D / 4
+// lanes each; with PW = 1 all groups share the parts of one pair.
+template <int D, bool BF16, int PW>
 __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int pairs) {
   constexpr int L4 = D / 4;          // lanes of a part
-  constexpr int kGroups = 256 / L4;
+  constexpr int kGroups = 256 / L4, kShare = kGroups / PW;
   __shared__ float s_m[kGroups], s_l[kGroups];
-  __shared__ f32x4 s_o[kGroups][L4];
-  const int64_t gp = blockIdx.x;
-  const int64_t row = gp / p.n_q_heads;
-  const int head = (int)(gp - row * p.n_q_heads), h = head / p.group;
-  const int seq = (int)(row / p.mx.rows_per_seq);
-  const int pair = (int)(row - (int64_t)seq * p.mx.rows_per_seq) * p.group + head - h * p.group;
-  const int rb = pair / pairs, j = pair - rb * pairs, sb = seq * p.blocks_per_seq + rb;
-  const int total = p.prefix[p.n_seqs * p.blocks_per_seq], n = workers(p.n_workers, total);
-  const int base = p.prefix[sb], steps = (p.prefix[sb + 1] - base) / p.mx.n_kv_heads;
-  const int t0 = base + h * steps, t1 = t0 + steps;
-  const int grp = threadIdx.x / L4, e = (threadIdx.x % L4) * 4;
+  __shared__ f32x4 s_o[kShare > 1 ? kGroups : 1][L4];
+  const int chunks = (min(pairs, p.mx.rows_per_seq * p.group) + PW - 1) / PW, hkv = p.mx.n_kv_heads;
+  const int sb = blockIdx.x / (chunks * hkv), rest = blockIdx.x - sb * (chunks * hkv);
+  const int h = rest / chunks, chunk = rest - h * chunks;
+  const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
+  const int grp = threadIdx.x / L4, share = grp / PW, e = (threadIdx.x % L4) * 4;
+  const int j = chunk * PW + grp % PW, pair = rb * pairs + j;
+  const bool out = pair < p.mx.rows_per_seq * p.group;
+  if (rb * pairs + chunk * PW >= p.mx.rows_per_seq * p.group) return;
+  const int base = p.prefix[sb], next = p.prefix[sb + 1], total = p.prefix[p.n_seqs * p.blocks_per_seq];
+  const int n = workers(p.n_workers, total), steps = (next - base) / hkv;
   float M = kMInit, L = 0.f;
   f32x4 o{};
   if (steps > 0) {
-    // the workgroup that holds step x is the last whose part begins at or before it
-    const int w0 = (int)((((int64_t)t0 + 1) * n - 1) / total), w1 = (int)(((int64_t)t1 * n - 1) / total);
+    // The workgroup that holds step x is the last whose part begins at or
+    // before it (doubles: exact below 2^53, quotients far from rounding up).
+    const int t0 = base + h * steps, t1 = t0 + steps;
+    const int w0 = (int)(((double)(t0 + 1) * n - 1) / total), w1 = (int)(((double)t1 * n - 1) / total);
     if (w0 == w1) return;  // written by that workgroup
-    for (int w = w0 + grp; w <= w1; w += kGroups) {
-      const int64_t slot = 2 * (int64_t)w + (part_begin(w, total, n) >= t0 ? 0 : 1);
-      const float2 ml = p.part_ml[slot * pairs + j];
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(p.part_o + (slot * pairs + j) * D + e);
-      const float mn = fmaxf(M, ml.x), a = fast_exp2(M - mn), b = fast_exp2(ml.x - mn);
+    const int first = 2 * w0 + (part_begin(w0, total, n) >= t0 ? 0 : 1);
+    if (out)
+      for (int w = w0 + share; w <= w1; w += kShare) {
+        const int64_t slot = w == w0 ? first : 2 * w;
+        const float2 ml = p.part_ml[slot * pairs + j];
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(p.part_o + (slot * pairs + j) * D + e);
+        const float mn = fmaxf(M, ml.x), a = fast_exp2(M - mn), b = fast_exp2(ml.x - mn);
+        M = mn;
+        L = L * a + ml.y * b;
+        o = o * a + x * b;
+      }
+  }
+  if constexpr (kShare > 1) {
+    s_o[grp][threadIdx.x % L4] = o;
+    if (e == 0) {
+      s_m[grp] = M;
+      s_l[grp] = L;
+    }
+    __syncthreads();
+    if (share) return;
+    for (int i = PW + grp; i < kGroups; i += PW) {
+      const float mn = fmaxf(M, s_m[i]), a = fast_exp2(M - mn), b = fast_exp2(s_m[i] - mn);
       M = mn;
-      L = L * a + ml.y * b;
-      o = o * a + x * b;
+      L = L * a + s_l[i] * b;
+      o = o * a + s_o[i][threadIdx.x % L4] * b;
     }
   }
-  s_o[grp][threadIdx.x % L4] = o;
-  if (e == 0) {
-    s_m[grp] = M;
-    s_l[grp] = L;
-  }
-  __syncthreads();
-  if (grp) return;
-  for (int i = 1; i < kGroups; ++i) {
-    const float mn = fmaxf(M, s_m[i]), a = fast_exp2(M - mn), b = fast_exp2(s_m[i] - mn);
-    M = mn;
-    L = L * a + s_l[i] * b;
-    o = o * a + s_o[i][threadIdx.x] * b;
-  }
+  if (!out) return;
   o *= L == 0.f ? 0.f : 1.f / L;
+  const int64_t gp = ((int64_t)seq * p.mx.rows_per_seq + pair / p.group) * p.n_q_heads + h * p.group + pair % p.group;
   if constexpr (BF16) {
-    ushort4 y = {f32_to_bf16(o[0]), f32_to_bf16(o[1]), f32_to_bf16(o[2]), f32_to_bf16(o[3])};
-    *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) = y;
+    *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
+        make_ushort4(f32_to_bf16(o[0]), f32_to_bf16(o[1]), f32_to_bf16(o[2]), f32_to_bf16(o[3]));
   } else {
     *reinterpret_cast<f32x4 *>(static_cast<float *>(p.o_out) + gp * D + e) = o;
   }
@@ -757,13 +807,24 @@ void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStre
   const int grid = p.n_workers ? p.n_workers : n_sb * p.mx.n_kv_heads;
   const size_t lds = p.n_workers ? (size_t)(n_sb + 1) * 4 : 0;
   if (sh.pairs > 32)
-    attn_mx_many_kernel<D, THICK_MT><<<grid, kThreads, lds, s>>>(p);
+    attn_mx_many_kernel<D><<<grid, kThreads, lds, s>>>(p);
   else if (bf16)
     sh.pairs > 16 ? attn_mx_kernel<D, 2, 1><<<grid, kThreads, lds, s>>>(p)
                   : attn_mx_kernel<D, 1, 1><<<grid, kThreads, lds, s>>>(p);
   else
     sh.pairs > 16 ? attn_mx_kernel<D, 2, 3><<<grid, kThreads, lds, s>>>(p)
                   : attn_mx_kernel<D, 1, 3><<<grid, kThreads, lds, s>>>(p);
+}
+
+template <int D, int PW>
+void launch_merge(const MxAttnParams &p, const MxAttnShape &sh, int blocks, bool few, bool bf16, hipStream_t s) {
+  const int pairs = std::min(sh.pairs, p.mx.rows_per_seq * p.group);  // of the largest block
+  const int grid = blocks * (few ? pairs : (pairs + PW - 1) / PW);
+  if (few)
+    bf16 ? attn_mx_merge_kernel<D, true, 1><<<grid, 256, 0, s>>>(p, sh.pairs)
+         : attn_mx_merge_kernel<D, false, 1><<<grid, 256, 0, s>>>(p, sh.pairs);
+  else
+    attn_mx_merge_kernel<D, true, PW><<<grid, 256, 0, s>>>(p, sh.pairs);
 }
 
 }  // namespace
@@ -773,12 +834,12 @@ MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_head
   MxAttnShape L{};
   const int64_t pairs = (int64_t)rows_per_seq * (n_q_heads / n_kv_heads);
   const bool many = bf16 && pairs > 32;
-  L.pairs = pairs <= 16 ? 16 : many ? 16 * THICK_MT * kWaves : 32;
+  L.pairs = pairs <= 16 ? 16 : many ? kManyPairs : 32;
   L.blocks_per_seq = (int32_t)((pairs + L.pairs - 1) / L.pairs);
   const int64_t n_sb = (int64_t)n_seqs * L.blocks_per_seq, blocks = n_sb * n_kv_heads;
   const int64_t steps = ((int64_t)n_ctx + kStep - 1) / kStep;
   const int64_t resident =
-      256 * (many ? THICK_OCC : waves_per_simd(head_dim, L.pairs > 16 ? 2 : 1, bf16 ? 1 : 3));
+      256 * (many ? 2 : waves_per_simd(head_dim, L.pairs > 16 ? 2 : 1, bf16 ? 1 : 3));
   // Workgroups share the steps out evenly while their parts can be listed and
   // there are steps to share; otherwise one workgroup takes a block.
   if (steps > 8 && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX)
@@ -803,13 +864,14 @@ hipError_t launch_attn_mx(const MxAttnParams &p, const MxAttnShape &sh, int head
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.n_workers) return e;
   ProfScope ps("attn_mx_merge", s);
-  const int64_t gp = (int64_t)p.n_seqs * p.mx.rows_per_seq * p.n_q_heads;
+  // Few pairs: many parts of each, shared out over a workgroup; many pairs: a
+  // few parts of each, one group of lanes.
+  const int blocks = p.n_seqs * p.blocks_per_seq * p.mx.n_kv_heads;
+  const bool few = sh.pairs <= 32;
   if (head_dim == 128)
-    bf16 ? attn_mx_merge_kernel<128, true><<<gp, 256, 0, s>>>(p, sh.pairs)
-         : attn_mx_merge_kernel<128, false><<<gp, 256, 0, s>>>(p, sh.pairs);
+    launch_merge<128, 8>(p, sh, blocks, few, bf16, s);
   else
-    bf16 ? attn_mx_merge_kernel<64, true><<<gp, 256, 0, s>>>(p, sh.pairs)
-         : attn_mx_merge_kernel<64, false><<<gp, 256, 0, s>>>(p, sh.pairs);
+    launch_merge<64, 16>(p, sh, blocks, few, bf16, s);
   return hipGetLastError();
 }
 
