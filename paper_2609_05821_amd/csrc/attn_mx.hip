@@ -27,9 +27,6 @@
 namespace conduit {
 namespace {
 
-#ifndef SCHED
-#define SCHED
-#endif
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kMInit = -1e30f;  // initial running maximum (log2 units)
 // The running maximum moves when a step exceeds it by more than this many log2
@@ -406,8 +403,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
       wave_lds_fence();
     };
 
-    // Two register sets take turns, so that a step is loaded while the one
-    // before it is used; its page is looked up one step earlier still.
+    // A step is loaded while the one before it is used; its page is looked up
+    // one step earlier still.  (Copied rather than unrolled into two register
+    // sets: code that runs once or twice costs its instruction fetches.)
     {
       Step<D> a, b;
       int key0 = first * kStep + wave * kWaveKeys;
@@ -421,18 +419,12 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
         entry = page_entry(pages, index(key0 + kStep));
         load_step<D>(p.mx, page_number(p.mx, pages, index(key0), now), h, key0, lane, a);
       }
-      auto load_next = [&](Step<D> &st) __attribute__((always_inline)) {
-        if (key0 + kStep < end)
-          load_step<D>(p.mx, page_number(p.mx, pages, index(key0 + kStep), entry), h, key0 + kStep, lane, st);
-        entry = page_entry(pages, index(key0 + 2 * kStep));
-      };
       while (key0 < end) {
-        load_next(b);
+        if (key0 + kStep < end)
+          load_step<D>(p.mx, page_number(p.mx, pages, index(key0 + kStep), entry), h, key0 + kStep, lane, b);
+        entry = page_entry(pages, index(key0 + 2 * kStep));
         use(a, key0);
-        key0 += kStep;
-        if (key0 >= end) break;
-        load_next(a);
-        use(b, key0);
+        a = b;
         key0 += kStep;
       }
     }
@@ -517,7 +509,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
   constexpr int VP = D + 16;
   constexpr int LPK = D / 32;                        // lanes of a key's values
   constexpr int VK = kTileKeys / kWaves;             // keys whose values a wave unpacks
-  __shared__ __attribute__((aligned(16))) u16 s_v[2][kTileKeys * VP];
+  __shared__ __attribute__((aligned(16))) u16 s_v[4][kTileKeys * VP];
   __shared__ int s_sum[kWaves];
   extern __shared__ int s_prefix[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -576,43 +568,53 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
       u32x4 v;
       int vs;
     };
-    auto slot_of = [&](int tile) __attribute__((always_inline)) {
-      return ((int64_t)h << c.shift) + ((min(tile, last - 1) * kTileKeys) & ((1 << c.shift) - 1));
+    // Where a tile begins in the code pools and in the scale pools.
+    struct Place {
+      int64_t codes, scales;
     };
-    auto load_keys = [&](int tile, int page, int half, Keys &x) __attribute__((always_inline)) {
-      const int64_t slot = slot_of(tile) + 32 * half;
-      const uint8_t *k = c.k + page * c.code_stride + slot * (D / 2) + col * (D / 2) + hh * (D / 4);
-      const uint8_t *ks = c.k_scale + page * c.scale_stride + slot * (D / kMxBlock) + col * (D / kMxBlock) +
-                          hh * (D / 2 / kMxBlock);
+    const int64_t head = (int64_t)h << c.shift;
+    auto place = [&](int tile, int page) __attribute__((always_inline)) {
+      const int64_t slot = head + ((min(tile, last - 1) * kTileKeys) & ((1 << c.shift) - 1));
+      return Place{page * c.code_stride + slot * (D / 2), page * c.scale_stride + slot * (D / kMxBlock)};
+    };
+    const uint32_t k_lane = col * (D / 2) + hh * (D / 4), ks_lane = col * (D / kMxBlock) + hh * (D / 2 / kMxBlock);
+    // (at head_dim 64 half of the lanes hold the wave's 16 keys)
+    const uint32_t v_lane4 = min(lane, VK * LPK - 1);
+    auto load_keys = [&](const Place &at, int half, Keys &x) __attribute__((always_inline)) {
+      const uint8_t *k = c.k + at.codes + half * (32 * (D / 2));
+      const uint8_t *ks = c.k_scale + at.scales + half * (32 * (D / kMxBlock));
 #pragma unroll
       for (int i = 0; i < C / 4; ++i) {
-        const u32x4 y = ld16(k + 16 * i);
+        const u32x4 y = ld16(k + k_lane + 16 * i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x.k[4 * i + e] = y[e];
       }
       if constexpr (D == 128)
-        x.ks = *reinterpret_cast<const uint16_t *>(ks);
+        x.ks = *reinterpret_cast<const uint16_t *>(ks + ks_lane);
       else
-        x.ks = *ks;
+        x.ks = ks[ks_lane];
     };
-    auto load_values = [&](int tile, int page, Values &x) __attribute__((always_inline)) {
-      const int64_t slot = slot_of(tile) + wave * VK;
-      // (at head_dim 64 half of the lanes hold the wave's 16 keys)
-      const int vl = min(lane, VK * LPK - 1);
-      x.v = ld16(c.v + page * c.code_stride + slot * (D / 2) + vl * 16);
-      x.vs = c.v_scale[page * c.scale_stride + slot * (D / kMxBlock) + vl];
+    auto load_values = [&](const Place &at, Values &x) __attribute__((always_inline)) {
+      const uint8_t *v = c.v + at.codes + wave * (VK * (D / 2));
+      const uint8_t *vs = c.v_scale + at.scales + wave * (VK * (D / kMxBlock));
+      x.v = ld16(v + v_lane4 * 16);
+      x.vs = vs[v_lane4];
     };
+    // A wave's 16 keys of a tile's values into LDS (of a tile past the last one: the
+    // last one's, into a buffer that is not read).
+    const int k16 = lane / LPK;
+    const uint32_t put_lane =
+        (wave * VK + 8 * ((k16 >> 2) & 1) + 2 * (k16 & 3) + ((k16 >> 3) & 1)) * VP + (lane % LPK) * 32;
     auto put_values = [&](int tile, Values &x) __attribute__((always_inline)) {
-      if (lane >= VK * LPK) return;
-      const int k16 = lane / LPK;                    // of the wave's 16 keys
       // keys past every row: their values must not reach the product as NaN or
       // infinity (their probabilities are 0)
       const bool hidden = tile * kTileKeys + wave * VK + k16 >= block_most;
-      const float s = scale_of(hidden ? 127 : x.vs);
-      const int row = 8 * ((k16 >> 2) & 1) + 2 * (k16 & 3) + (k16 >> 3);
-      u16 *dst = s_v[tile & 1] + (wave * VK + row) * VP + (lane % LPK) * 32;
+      const float sc = scale_of(hidden ? 127 : x.vs);
+      u16 *dst = s_v[tile & 3] + put_lane;
+      if (VK * LPK == 64 || lane < VK * LPK) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) st16(dst + 8 * i, __builtin_bit_cast(u32x4, unpack8(hidden ? 0 : x.v[i], s)));
+        for (int i = 0; i < 4; ++i) st16(dst + 8 * i, __builtin_bit_cast(u32x4, unpack8(hidden ? 0 : x.v[i], sc)));
+      }
     };
     const SeqPages pages = seq_pages(c, seq);
     auto index = [&](int tile) __attribute__((always_inline)) { return min(tile, last - 1) * kTileKeys >> c.shift; };
@@ -622,85 +624,120 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
     auto key_operand = [&](const Keys &x, int d) __attribute__((always_inline)) {
       return unpack8(x.k[d], scale_of(d < 4 ? x.ks & 0xff : x.ks >> 8));
     };
-    // Softmax and O^T products of 32 keys whose S^T is in s, with the S^T products
-    // of the next 32 (nx) between them, so that matrix and vector work of one
-    // wave overlap.
-    auto half_step = [&](int tile, int half, f32x16 &s, const Keys &nx) __attribute__((always_inline)) {
-      const int key0 = tile * kTileKeys + 32 * half;
-      if (key0 + 32 > least) {
+    auto largest = [&](const f32x16 &s) __attribute__((always_inline)) {
+      float t[5];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = key0 + (i & 3) + 8 * (i >> 2) + 4 * hh < seen ? s[i] : kNegInf;
-      }
-      float top = s[0];
+      for (int i = 0; i < 5; ++i) t[i] = fmaxf(fmaxf(s[3 * i], s[3 * i + 1]), s[3 * i + 2]);
+      return fmaxf(fmaxf(fmaxf(t[0], t[1]), t[2]), fmaxf(fmaxf(t[3], t[4]), s[15])) * p.scale_log2;  // (scale > 0)
+    };
+    // S^T of 32 keys and the lane's largest (in the log2 domain).
+    struct Scores {
+      f32x16 s;
+      float top;
+    };
+    auto products = [&](const Keys &x) __attribute__((always_inline)) {
+      f32x16 s{};
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      top *= p.scale_log2;  // (the scale is positive)
-      if (__any(top > m + kSlack)) {
-        const float mn = fmaxf(m, half_max(top)), a = fast_exp2(m - mn);
+      for (int d = 0; d < C; ++d) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(x, d), q[d], s, 0, 0, 0);
+      return s;
+    };
+    // The keys from key0 on that the row does not see.
+    auto mask = [&](int key0, Scores &x) __attribute__((always_inline)) {
+      if (key0 + 32 <= least) return;
+      const int limit = seen - key0 - 4 * hh;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x.s[i] = (i & 3) + 8 * (i >> 2) < limit ? x.s[i] : kNegInf;
+      x.top = largest(x.s);
+    };
+    // Softmax and O^T products of 32 keys whose S^T is in x, and the S^T products of
+    // the next 32 (nx), in one block of code without branches, so that matrix and
+    // vector work of one wave overlap; `extra` joins them.
+    auto half_step = [&](int tile, int half, Scores &x, const Keys &nx, auto &&extra) __attribute__((always_inline)) {
+      if (__any(x.top > m + kSlack)) {
+        const float mn = fmaxf(m, half_max(x.top)), a = fast_exp2(m - mn);
         m = mn;
         l *= a;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] *= a;
       }
-      f32x16 sn{};
+      const u16 *at = s_v[tile & 3] + 32 * half * VP + v_lane;
+      bf16x8 v0[DT];
 #pragma unroll
-      for (int d = 0; d < C; ++d) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(nx, d), q[d], sn, 0, 0, 0);
+      for (int dt = 0; dt < DT; ++dt) v0[dt] = v_operand_il<VP>(at + 32 * dt);
+      const f32x16 sn = products(nx);
       bf16x8 pr[2];
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float e = fast_exp2(__builtin_fmaf(s[i], p.scale_log2, -m));
-        l += e;
+        const float e = fast_exp2(__builtin_fmaf(x.s[i], p.scale_log2, -m));
+        sum[i & 1] += e;
         pr[i >> 3][i & 7] = static_cast<__bf16>(e);
       }
-      const u16 *at = s_v[tile & 1] + 32 * half * VP + v_lane;
+      l += sum[0] + sum[1];
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+      for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[dt], pr[0], o[dt], 0, 0, 0);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand_il<VP>(at + 16 * kk * VP + 32 * dt), pr[kk], o[dt],
-                                                          0, 0, 0);
-      SCHED
-      s = sn;
+      for (int dt = 0; dt < DT; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand_il<VP>(at + 16 * VP + 32 * dt), pr[1], o[dt], 0, 0, 0);
+      x.s = sn;
+      x.top = largest(sn);
+      extra();
     };
-    // A tile: S^T of its first half is in s, its second half's keys are in b, the
-    // next tile's in c0 and d (loaded two half steps before their use).
-    int page1 = 0, entry2 = 0;  // the next tile's page, the table entry of the one after
-    auto tile_step = [&](int tile, f32x16 &s, Keys &a, Keys &b, Keys &c0, Keys &d) __attribute__((always_inline)) {
+    // A tile: S^T of its first half is in x, its second half's keys are in b, the
+    // next tile's in c0 and d (loaded two half steps before their use).  Values go
+    // two tiles ahead into LDS, so that the waves meet every second tile only.
+    Place at1, at2;  // the next two tiles
+    int entry3 = 0;  // the table entry of the one after
+    auto tile_step = [&](int tile, Scores &x, Keys &a, Keys &b, Keys &c0, Keys &d) __attribute__((always_inline)) {
       Values v;
-      load_values(tile + 1, page1, v);
-      load_keys(tile + 1, page1, 1, d);
-      const int entry3 = page_entry(pages, index(tile + 3));
+      load_values(at2, v);
+      load_keys(at1, 1, d);
+      const int entry4 = page_entry(pages, index(tile + 4));
       const bool active = tile * kTileKeys < most;
-      if (active) half_step(tile, 0, s, b);
-      page1 = page_of(tile + 2, entry2);
-      entry2 = entry3;
-      load_keys(tile + 2, page1, 0, a);
-      if (active) half_step(tile, 1, s, c0);
-      if (tile + 1 < last) put_values(tile + 1, v);
-      __syncthreads();
+      if (active) {
+        half_step(tile, 0, x, b, [] {});
+        mask(tile * kTileKeys + 32, x);
+      }
+      load_keys(at2, 0, a);
+      at1 = at2;
+      at2 = place(tile + 3, page_of(tile + 3, entry3));
+      entry3 = entry4;
+      if (active) {
+        half_step(tile, 1, x, c0, [&] { put_values(tile + 2, v); });
+        mask(tile * kTileKeys + 64, x);
+      } else {
+        put_values(tile + 2, v);
+      }
     };
 
     if (sg.first < last) {
       Keys k0, k1, k2, k3;
-      f32x16 s{};
+      Scores x;
       {
-        const int entry0 = page_entry(pages, index(sg.first)), entry1 = page_entry(pages, index(sg.first + 1));
-        entry2 = page_entry(pages, index(sg.first + 2));
-        const int page = page_of(sg.first, entry0);
-        Values v;
-        load_values(sg.first, page, v);
-        load_keys(sg.first, page, 0, k0);
-        load_keys(sg.first, page, 1, k1);
-        page1 = page_of(sg.first + 1, entry1);
-        load_keys(sg.first + 1, page1, 0, k2);
-        put_values(sg.first, v);
+        int entry[3];
 #pragma unroll
-        for (int d = 0; d < C; ++d) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(k0, d), q[d], s, 0, 0, 0);
+        for (int i = 0; i < 3; ++i) entry[i] = page_entry(pages, index(sg.first + i));
+        entry3 = page_entry(pages, index(sg.first + 3));
+        const Place at0 = place(sg.first, page_of(sg.first, entry[0]));
+        at1 = place(sg.first + 1, page_of(sg.first + 1, entry[1]));
+        at2 = place(sg.first + 2, page_of(sg.first + 2, entry[2]));
+        Values v, v1;
+        load_values(at0, v);
+        load_values(at1, v1);
+        load_keys(at0, 0, k0);
+        load_keys(at0, 1, k1);
+        load_keys(at1, 0, k2);
+        put_values(sg.first, v);
+        put_values(sg.first + 1, v1);
+        x.s = products(k0);
+        x.top = largest(x.s);
+        mask(sg.first * kTileKeys, x);
       }
       __syncthreads();
       for (int tile = sg.first; tile < last; tile += 2) {
-        tile_step(tile, s, k0, k1, k2, k3);
-        if (tile + 1 < last) tile_step(tile + 1, s, k2, k3, k0, k1);
+        tile_step(tile, x, k0, k1, k2, k3);
+        if (tile + 1 < last) tile_step(tile + 1, x, k2, k3, k0, k1);
+        __syncthreads();
       }
     }
 
