@@ -655,11 +655,12 @@ def conduit_attn_mx(mx: KVMX, q: torch.Tensor, pos: torch.Tensor, o_out: torch.T
         raise ConduitError(ERR_INVALID_ARG, "lse_out must be dense float32 [n, H_q]")
     if scale is None:
         scale = 1.0 / math.sqrt(mx.head_dim)
-    need = attn_mx_workspace_bytes(mx, q)
-    if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-        if stream is not None:
-            ws.record_stream(stream)  # freed on return, used on that stream
+    if ws is None:
+        need = attn_mx_workspace_bytes(mx, q)
+        if need:
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            if stream is not None:
+                ws.record_stream(stream)  # freed on return, used on that stream
     _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws), stream, ctypes.byref(mx), _ptr(q),
           _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
 

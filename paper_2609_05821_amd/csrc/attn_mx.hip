@@ -232,15 +232,23 @@ __device__ __forceinline__ void load_step(const MxCache &c, int64_t page, int h,
   }
 }
 
-// Waves a SIMD holds (workgroups a CU holds) of each variant, by its registers.
+// Waves a SIMD holds (workgroups of 4 waves a CU holds) of each variant, by its
+// registers.
 constexpr int waves_per_simd(int D, int MT, int NS) {
-  return D == 128 ? (MT == 1 && NS == 1 ? 3 : MT == 2 && NS == 3 ? 1 : 2) : (MT == 1 ? 3 : 2);
+  return D == 128 ? (MT == 1 && NS == 1 ? 3 : 2) : (MT == 1 ? (NS == 1 ? 4 : 3) : NS == 1 ? 3 : 2);
 }
+// Pairs of a block with few pairs: 32 read the cache once for twice as many, but
+// fp32 rows of 128 dims would leave registers for one wave per SIMD only (1,500
+// rows over 16k tokens: 32 pairs 1,094 us, 16 pairs 823 us).
+constexpr int few_pairs(int D, int64_t pairs, bool bf16) { return pairs <= 16 || (D == 128 && !bf16) ? 16 : 32; }
 
 // MT: groups of 16 pairs of a block.  NS: exact bf16 parts of queries and
-// probabilities (1: bf16 tensors, 3: fp32).
-template <int D, int MT, int NS>
-__global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_kernel(MxAttnParams p) {
+// probabilities (1: bf16 tensors, 3: fp32).  W: waves of a workgroup, 4, or 8 for a
+// workgroup per block on up to 256 blocks (64 sequences of 2,048 keys: 4 waves 20
+// us, 8 waves 15 us; 256 of 512, which leave the CUs several blocks each: 16 and 25 us).
+template <int D, int MT, int NS, int W>
+__global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_kernel(MxAttnParams p) {
+  constexpr int kWaves = W, kStep = W * kWaveKeys;
   constexpr int kPairs = 16 * MT;
   constexpr int C = D / 32;            // MFMA steps over the dims
   constexpr int DT = D / 16;           // 16-dim tiles of O^T
@@ -273,6 +281,23 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
     const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
     const int n_pairs = min(kPairs, r * G - rb * kPairs);
     const int64_t row_base = (int64_t)seq * r;
+
+    // The wave's first step is on its way before anything else is (positions past
+    // the rows' last key are masked, those past the cache are not loaded).
+    const SeqPages pages = seq_pages(p.mx, seq);
+    auto index = [&](int key) __attribute__((always_inline)) { return min(key, p.mx.n_ctx - 1) >> p.mx.shift; };
+    auto load = [&](int key, int entry, Step<D> &st) __attribute__((always_inline)) {
+      const int at = min(key, (p.mx.n_ctx - 1) & ~(kWaveKeys - 1));
+      load_step<D>(p.mx, page_number(p.mx, pages, index(at), entry), h, at, lane, st);
+    };
+    Step<D> st[2];
+    int key0 = first * kStep + wave * kWaveKeys;
+    int entry = page_entry(pages, index(key0));
+    {
+      const int next = page_entry(pages, index(key0 + kStep));
+      load(key0, entry, st[0]);
+      entry = next;  // of the next step to load
+    }
 
     // Queries and key counts of the lane's columns.  Columns past the block
     // see every key (nothing to mask) and are not written.
@@ -403,33 +428,24 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
       wave_lds_fence();
     };
 
-    // A step is loaded while the one before it is used; its page is looked up
-    // one step earlier still.  (Copied rather than unrolled into two register
-    // sets: code that runs once or twice costs its instruction fetches.)
+    // Two register sets take turns: a step is loaded while the one before it is used
+    // (two steps ahead gain nothing), its page looked up one step earlier still.
     {
-      Step<D> a, b;
-      int key0 = first * kStep + wave * kWaveKeys;
       const int end = min(most, last * kStep);  // (last * kStep < n_ctx + kStep <= 2^30 + kStep)
-      // page of key `key`, or of the last key
-      auto index = [&](int key) __attribute__((always_inline)) { return min(key, end - 1) >> p.mx.shift; };
-      const SeqPages pages = seq_pages(p.mx, seq);
-      int entry = 0;
-      if (key0 < end) {
-        const int now = page_entry(pages, index(key0));
-        entry = page_entry(pages, index(key0 + kStep));
-        load_step<D>(p.mx, page_number(p.mx, pages, index(key0), now), h, key0, lane, a);
-      }
-      while (key0 < end) {
-        if (key0 + kStep < end)
-          load_step<D>(p.mx, page_number(p.mx, pages, index(key0 + kStep), entry), h, key0 + kStep, lane, b);
+      auto turn = [&](Step<D> &now, Step<D> &next) __attribute__((always_inline)) {
+        if (key0 + kStep < end) load(key0 + kStep, entry, next);
         entry = page_entry(pages, index(key0 + 2 * kStep));
-        use(a, key0);
-        a = b;
+        use(now, key0);
         key0 += kStep;
+      };
+      while (key0 < end) {
+        turn(st[0], st[1]);
+        if (key0 >= end) break;
+        turn(st[1], st[0]);
       }
     }
 
-    // The four waves' results, 16 pairs at a time.
+    // The waves' results, 16 pairs at a time.
     const bool whole = !p.n_workers || (first == 0 && last == sg.steps);
     const int slot = 2 * blockIdx.x + (t == part0 ? 0 : 1);
 #pragma unroll
@@ -447,7 +463,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, MT, NS)) void attn_mx_k
         *reinterpret_cast<f32x4 *>(tile_o + col * OP + 16 * dt + 4 * g) = o[mt][dt];
       __syncthreads();
       const int j = tid >> 4, pair = rb * kPairs + 16 * mt + j;
-      if (16 * mt + j < n_pairs) {
+      if (j < 16 && 16 * mt + j < n_pairs) {
         float M = s_m[0][j], L = 0.f, a[kWaves];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][j]);
@@ -838,6 +854,17 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int 
   if (e == 0 && p.lse_out) p.lse_out[gp] = L == 0.f ? kNegInf : (M + __log2f(L)) * kLn2;
 }
 
+template <int D, int W>
+void launch_few(const MxAttnParams &p, bool wide, bool bf16, int grid, size_t lds, hipStream_t s) {
+  if (bf16)
+    wide ? attn_mx_kernel<D, 2, 1, W><<<grid, 64 * W, lds, s>>>(p)
+         : attn_mx_kernel<D, 1, 1, W><<<grid, 64 * W, lds, s>>>(p);
+  else if (!wide)
+    attn_mx_kernel<D, 1, 3, W><<<grid, 64 * W, lds, s>>>(p);
+  else if constexpr (few_pairs(D, 32, false) == 32)
+    attn_mx_kernel<D, 2, 3, W><<<grid, 64 * W, lds, s>>>(p);
+}
+
 template <int D>
 void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStream_t s) {
   const int n_sb = p.n_seqs * p.blocks_per_seq;
@@ -845,12 +872,10 @@ void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStre
   const size_t lds = p.n_workers ? (size_t)(n_sb + 1) * 4 : 0;
   if (sh.pairs > 32)
     attn_mx_many_kernel<D><<<grid, kThreads, lds, s>>>(p);
-  else if (bf16)
-    sh.pairs > 16 ? attn_mx_kernel<D, 2, 1><<<grid, kThreads, lds, s>>>(p)
-                  : attn_mx_kernel<D, 1, 1><<<grid, kThreads, lds, s>>>(p);
+  else if (p.n_workers || grid > 256)
+    launch_few<D, 4>(p, sh.pairs > 16, bf16, grid, lds, s);
   else
-    sh.pairs > 16 ? attn_mx_kernel<D, 2, 3><<<grid, kThreads, lds, s>>>(p)
-                  : attn_mx_kernel<D, 1, 3><<<grid, kThreads, lds, s>>>(p);
+    launch_few<D, 8>(p, sh.pairs > 16, bf16, grid, lds, s);
 }
 
 template <int D, int PW>
@@ -871,15 +896,20 @@ MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_head
   MxAttnShape L{};
   const int64_t pairs = (int64_t)rows_per_seq * (n_q_heads / n_kv_heads);
   const bool many = bf16 && pairs > 32;
-  L.pairs = pairs <= 16 ? 16 : many ? kManyPairs : 32;
+  L.pairs = many ? kManyPairs : few_pairs(head_dim, pairs, bf16);
   L.blocks_per_seq = (int32_t)((pairs + L.pairs - 1) / L.pairs);
   const int64_t n_sb = (int64_t)n_seqs * L.blocks_per_seq, blocks = n_sb * n_kv_heads;
   const int64_t steps = ((int64_t)n_ctx + kStep - 1) / kStep;
   const int64_t resident =
       256 * (many ? 2 : waves_per_simd(head_dim, L.pairs > 16 ? 2 : 1, bf16 ? 1 : 3));
-  // Workgroups share the steps out evenly while their parts can be listed and
-  // there are steps to share; otherwise one workgroup takes a block.
-  if (steps > 8 && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX)
+  // Workgroups share the steps out evenly, for a second launch that merges, from
+  // this many steps of a block on (and while the parts' list fits LDS): fewer are
+  // done sooner by a workgroup per block, and the more blocks there are the less
+  // there is to even out.  One sequence of 4 KV heads: 1,024 keys 9 us by block,
+  // 13 us shared; 2,200 keys 14 and 12 us.  64 sequences of up to 2,048: 15 and 22
+  // us.  256 of up to 4,096: 73 and 84 us, of up to 8,192: 142 and 137 us.
+  const int64_t from = many || blocks < 256 ? 8 : blocks < 1024 ? 16 : 32;
+  if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX)
     L.n_workers = (int32_t)std::min<int64_t>(resident, std::max<int64_t>(1, blocks * steps / kMinSteps));
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
@@ -904,7 +934,7 @@ hipError_t launch_attn_mx(const MxAttnParams &p, const MxAttnShape &sh, int head
   // Few pairs: many parts of each, shared out over a workgroup; many pairs: a
   // few parts of each, one group of lanes.
   const int blocks = p.n_seqs * p.blocks_per_seq * p.mx.n_kv_heads;
-  const bool few = sh.pairs <= 32;
+  const bool few = sh.pairs <= 32 || p.n_workers > 4 * blocks;
   if (head_dim == 128)
     launch_merge<128, 8>(p, sh, blocks, few, bf16, s);
   else

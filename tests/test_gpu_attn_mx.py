@@ -210,6 +210,39 @@ def test_many_rows(dtype):
     check(st, q, mixed, o, lse, rows=[0, 7, 300, 699])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("r", [1, 25])
+def test_a_workgroup_per_block(dtype, d, r):
+    """More blocks than CUs, short caches: every block by one workgroup."""
+    n = 300
+    st = Store(n, 260, 3, 1, d, page=64, seed=21)
+    g = torch.Generator().manual_seed(4)
+    pos = torch.randint(-1, 260, (n * r,), generator=g, dtype=torch.int32)
+    q = queries(n * r, 3, d, dtype, 5)
+    o, lse = run(st, q, pos)
+    for s in (0, 1, 63, 150, 298, 299):
+        p = pos[s * r:(s + 1) * r]
+        m = max(int(p.max()) + 1, 0)
+        k, v = st.rows(s, m)
+        want = M.attention(q[s * r:(s + 1) * r], k, v, p)
+        bo, bl = M.attention_bounds(*want, m, d, dtype == "bf16")
+        assert ((o[s * r:(s + 1) * r].double() - want[0]).abs() <= bo).all()
+        live = p >= 0
+        assert ((lse[s * r:(s + 1) * r].double() - want[1]).abs()[live] <= bl[live]).all()
+        assert (lse[s * r:(s + 1) * r][~live] == -math.inf).all()
+
+
+def test_many_rows_of_small_heads():
+    """Heads of 64 dims, as many blocks as merge by groups of pairs."""
+    ctx, hq, hkv, d, r = 1500, 32, 8, 64, 600
+    st = Store(1, ctx, hq, hkv, d, seed=22)
+    pos = torch.randperm(ctx, generator=torch.Generator().manual_seed(3))[:r].sort().values.to(torch.int32)
+    q = queries(r, hq, d, "bf16", 6)
+    o, lse = run(st, q, pos)
+    check(st, q, pos, o, lse, rows=[0, 1, 31, 32, 33, 300, 567, 599])
+
+
 def test_many_sequences():
     """More sequence blocks than the list of parts holds: one workgroup per block."""
     n = 4500
