@@ -530,6 +530,8 @@ conduit_status conduit_append_kv(const conduit_kv *kv, const conduit_rows *rows,
  * cache of rows->dtype would hold it.  A token that has an infinity or a NaN
  * among its keys or values of some head is stored with scale byte 255 (NaN) in
  * that head's keys and zero values: rows that attend to it are NaN there.
+ * Value scale bytes above 252, which no append writes, are read as 252 by
+ * conduit_attn_mx.
  *
  * Pools: page p holds [n_kv_heads][page_size][head_dim / 2] code bytes (dim 2i in
  * the low four bits) at k + p * code_stride, and [n_kv_heads][page_size]
@@ -598,6 +600,8 @@ conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, 
  *           read no key past n_ctx - 1 (the row's output is then meaningless).
  *           Keys past a row's position do not enter its output, whatever they
  *           hold.
+ * scale     finite, > 0; |scale * q.k| below 2^30 for every key that a row attends
+ *           to (the row is meaningless otherwise).
  * o_out     device [n][n_q_heads][head_dim], dtype.
  * lse_out   nullable device [n][n_q_heads] fp32: natural-log log-sum-exp.
  * ws        conduit_attn_mx_workspace_bytes(mx, n, dtype) bytes, 256-byte aligned

@@ -70,6 +70,11 @@ __device__ __forceinline__ bf16x8 unpack8(uint32_t codes, float scale) {
 
 __device__ __forceinline__ float scale_of(int byte) { return __builtin_bit_cast(float, (uint32_t)byte << 23); }
 
+// Values stay finite whatever the pool holds (appends write no byte above this
+// one): a key that a row does not see has probability 0 there, and 0 times a NaN
+// or an infinity would reach its output.
+__device__ __forceinline__ float value_scale(int byte) { return scale_of(min(byte, kMxScaleMax)); }
+
 // Orders this wave's LDS writes before its reads (and the other way round) for
 // the compiler; the hardware keeps a wave's LDS accesses in order.
 __device__ __forceinline__ void wave_lds_fence() {
@@ -269,12 +274,13 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
   float *tile_o = reinterpret_cast<float *>(s_tile[wave]);
 
   // This workgroup's part [t, t_end) of the step list, or block blockIdx.x.
+  const bool shared = W == 4 && p.n_workers;
   int t = 0, t_end = 1;
-  if (p.n_workers && !plan_part(p, kPairs, kStep, s_sum, s_prefix, t, t_end)) return;
+  if (shared && !plan_part(p, kPairs, kStep, s_sum, s_prefix, t, t_end)) return;
   const int part0 = t;
 
   while (t < t_end) {
-    const Segment sg = p.n_workers ? segment_at(p, n_sb, s_prefix, t, t_end)
+    const Segment sg = shared ? segment_at(p, n_sb, s_prefix, t, t_end)
                                    : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0};
     const int sb = sg.sb, h = sg.h, first = sg.first;
     int last = sg.last;
@@ -349,20 +355,10 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
     auto use = [&](Step<D> &st, int key0) __attribute__((always_inline)) {
       // values: a lane's 16 bytes are one block of one key
       constexpr int LPK = D / 32;  // lanes of a key
-      if (key0 + kWaveKeys > most) {
-        // keys past every row of the block: their values must not reach the
-        // product as NaN or infinity (their probabilities are 0)
-#pragma unroll
-        for (int i = 0; i < Step<D>::kVL; ++i)
-          if (key0 + i * (64 / LPK) + lane / LPK >= most) {
-            st.v[i] = u32x4{};
-            st.vs[i] = 127;
-          }
-      }
 #pragma unroll
       for (int i = 0; i < Step<D>::kVL; ++i) {
         u16 *dst = tile + (i * (64 / LPK) + lane / LPK) * VP + (lane % LPK) * 32;
-        const float s = scale_of(st.vs[i]);
+        const float s = value_scale(st.vs[i]);
 #pragma unroll
         for (int x = 0; x < 4; ++x) st16(dst + 8 * x, __builtin_bit_cast(u32x4, unpack8(st.v[i][x], s)));
       }
@@ -446,7 +442,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
     }
 
     // The waves' results, 16 pairs at a time.
-    const bool whole = !p.n_workers || (first == 0 && last == sg.steps);
+    const bool whole = !shared || (first == 0 && last == sg.steps);
     const int slot = 2 * blockIdx.x + (t == part0 ? 0 : 1);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -500,7 +496,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
       }
     }
     __syncthreads();  // the tiles are free again
-    if (!p.n_workers) break;
+    if (!shared) break;
     t += last - first;
   }
 }
@@ -622,14 +618,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
     const uint32_t put_lane =
         (wave * VK + 8 * ((k16 >> 2) & 1) + 2 * (k16 & 3) + ((k16 >> 3) & 1)) * VP + (lane % LPK) * 32;
     auto put_values = [&](int tile, Values &x) __attribute__((always_inline)) {
-      // keys past every row: their values must not reach the product as NaN or
-      // infinity (their probabilities are 0)
-      const bool hidden = tile * kTileKeys + wave * VK + k16 >= block_most;
-      const float sc = scale_of(hidden ? 127 : x.vs);
+      const float sc = value_scale(x.vs);
       u16 *dst = s_v[tile & 3] + put_lane;
       if (VK * LPK == 64 || lane < VK * LPK) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) st16(dst + 8 * i, __builtin_bit_cast(u32x4, unpack8(hidden ? 0 : x.v[i], sc)));
+        for (int i = 0; i < 4; ++i) st16(dst + 8 * i, __builtin_bit_cast(u32x4, unpack8(x.v[i], sc)));
       }
     };
     const SeqPages pages = seq_pages(c, seq);

@@ -243,6 +243,29 @@ def test_many_rows_of_small_heads():
     check(st, q, pos, o, lse, rows=[0, 1, 31, 32, 33, 300, 567, 599])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("r", [2, 60])
+def test_keys_past_a_row_hold_anything(dtype, d, r):
+    """Rows of one block at tokens 99 and 600, whatever bytes follow token 99."""
+    st = Store(1, 640, 4, 2, d, page=64, seed=23)
+    g = torch.Generator().manual_seed(8)
+    k, v = st.rows(0, 100)
+    for t in range(100, 640):
+        at = int(st.table[0, t // 64])
+        for i in (2, 3):
+            st.cpu[i][at, :, t % 64] = torch.randint(0, 256, (2, d // 32), generator=g, dtype=torch.uint8)
+            st.cpu[i][at, :, t % 64, t % (d // 32)] = 255
+    st.upload()
+    pos = torch.tensor([99, 600] * (r // 2), dtype=torch.int32)
+    q = queries(r, 4, d, dtype, 9)
+    o, lse = run(st, q, pos)
+    want = M.attention(q[::2], k, v, pos[::2])
+    bo, bl = M.attention_bounds(*want, 100, d, dtype == "bf16")
+    assert ((o[::2].double() - want[0]).abs() <= bo).all()
+    assert ((lse[::2].double() - want[1]).abs() <= bl).all()
+
+
 def test_many_sequences():
     """More sequence blocks than the list of parts holds: one workgroup per block."""
     n = 4500
