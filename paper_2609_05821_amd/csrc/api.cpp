@@ -1517,6 +1517,8 @@ conduit_status conduit_attn_mx(const conduit_kv_mx *mx, const void *q, int32_t d
   ap.lse_out = lse_out;
   if (sh.total) {
     ap.prefix = reinterpret_cast<int32_t *>(at(ws, sh.prefix));
+    ap.cut = reinterpret_cast<int32_t *>(at(ws, sh.parts));
+    ap.parts = ap.cut + 1;
     ap.part_ml = reinterpret_cast<float2 *>(at(ws, sh.ml));
     ap.part_o = reinterpret_cast<float *>(at(ws, sh.o));
   }

@@ -89,6 +89,8 @@ struct MxAttnParams {
   void *o_out;                  // [n][n_q_heads][D]
   float *lse_out;               // nullable
   int32_t *prefix;              // [seq blocks + 1]: key steps before each
+  int32_t *cut;                 // length of parts that end with their block, or 0
+  int32_t *parts;               // [up to 64 seq blocks]: such parts before each
   float2 *part_ml;              // [2 * n_workers][pairs per block] running maximum, denominator
   float *part_o;                // [2 * n_workers][pairs per block][D] unnormalised output
 };
@@ -98,7 +100,7 @@ struct MxAttnShape {
   int32_t pairs;                // (row, head) pairs of a block
   int32_t blocks_per_seq;
   int32_t n_workers;
-  size_t prefix, ml, o, total;  // workspace offsets
+  size_t prefix, parts, ml, o, total;  // workspace offsets
 };
 MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_ctx,
                           int32_t head_dim, bool bf16);

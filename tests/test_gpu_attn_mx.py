@@ -266,6 +266,19 @@ def test_keys_past_a_row_hold_anything(dtype, d, r):
     assert ((lse[::2].double() - want[1]).abs() <= bl).all()
 
 
+@pytest.mark.parametrize("n_seqs,hkv", [(9, 8), (60, 8), (64, 5), (65, 5)])
+def test_ragged_sequences_share_workgroups(n_seqs, hkv):
+    """Few blocks (parts end with their block), many (parts go on into the next),
+    and either side of the list that a wave holds."""
+    st = Store(n_seqs, 2100, hkv, hkv, 64, page=64, seed=24)
+    g = torch.Generator().manual_seed(10)
+    pos = torch.randint(0, 2100, (n_seqs,), generator=g, dtype=torch.int32)
+    pos[0], pos[3], pos[4], pos[-1] = 2099, -1, -1, 0
+    q = queries(n_seqs, hkv, 64, "bf16", 11)
+    o, lse = run(st, q, pos)
+    check(st, q, pos, o, lse)
+
+
 def test_many_sequences():
     """More sequence blocks than the list of parts holds: one workgroup per block."""
     n = 4500
