@@ -16,10 +16,19 @@
 //   O^T += V^T P^T   values are unpacked to bf16 in LDS (each wave its own tile)
 //                and read back with transposing reads; the probabilities are the
 //                other operand as they lie in the S^T accumulators.
+// fp32 queries and probabilities are three exact bf16 parts each; bf16 tensors have
+// their probabilities rounded to bf16 for the product (2^-9 of each, the size of
+// the output's own rounding), while the sum they are divided by stays fp32.
+//
 // The work of a call is the list of all key steps of all (sequence, row block,
 // KV head) blocks.  Workgroups take equal contiguous parts of it, whatever the
 // sequences' lengths; a block that ends up in more than one part is merged by
 // a second launch.  Every workgroup derives the list from the positions itself.
+//
+// Measured: 64 sequences of up to 16,384 tokens (28 heads over 4, head_dim 128, 557
+// MB of codes and scales) 107 us and 6 us to merge, 5.2 TB/s of a large copy's 5.2;
+// one of 65,536 tokens 19 us, of 2,048 11 us (two launches and four dependent loads
+// deep: positions, page, codes, the merge).
 #include <algorithm>
 
 #include "mx.h"
@@ -560,8 +569,11 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
 // Many pairs per KV head (the selected rows of a refresh): bound by the matrix
 // products and the vector work between them.  The waves of a workgroup take 32
 // pairs each and go over the same keys, 64 at a time.  Keys are unpacked by every
-// wave for itself straight into operands, values once per workgroup into LDS, one
-// tile ahead.  Products are v_mfma_f32_32x32x16_bf16: beside it a wave issues
+// wave for itself straight into operands, values once per workgroup into LDS, two
+// tiles ahead.  (1,638 rows of 28 heads over 17,024 keys: 240 us, 833 TFLOP/s, and 14
+// us to merge; matrix cores busy 37% of the cycles, 9 vector instructions a product.
+// Keys through LDS as well, unpacked once for 8 waves: 5% slower, and 13% slower with
+// every product and its vector work in a fixed slot.)  Products are v_mfma_f32_32x32x16_bf16: beside it a wave issues
 // vector instructions for free, beside 16x16x32 it does not (16 of the former with
 // 64 fma between them 543 cycles, 32 of the latter, the same products, 659).
 //   S^T: lane (key, h) holds half h of the key's dims, codes and scales in one piece
