@@ -562,8 +562,9 @@ def _rope_args(rope: Optional[Rope], rope_pos: Optional[torch.Tensor], n: int):
         return None, None, 0
     if rope_pos.dim() == 1:
         rope_pos = rope_pos[None]
-    if rope_pos.dtype != torch.int32 or rope_pos.shape != (rope.n_axes, n) or (n > 1 and rope_pos.stride(1) != 1):
-        raise ConduitError(ERR_INVALID_ARG, f"rope_pos must be int32 [{rope.n_axes}, {n}], rows dense")
+    if rope_pos.dtype != torch.int32 or rope_pos.shape != (rope.n_axes, n) or (n > 1 and rope_pos.stride(1) != 1) or \
+            (rope.n_axes > 1 and rope_pos.stride(0) < n):
+        raise ConduitError(ERR_INVALID_ARG, f"rope_pos must be int32 [{rope.n_axes}, {n}], rows dense and apart")
     return ctypes.byref(rope.desc), rope_pos.data_ptr(), max(rope_pos.stride(0), n)
 
 

@@ -289,3 +289,11 @@ def test_attention_by_hand():
     assert torch.allclose(o[:, 0, 0], torch.tensor([2.0, 5.0, 0.0], dtype=torch.float64))
     assert torch.allclose(lse[:2, 1], torch.tensor([0.0, math.log(4.0)], dtype=torch.float64))
     assert lse[2, 0] == -math.inf
+
+
+@pytest.mark.parametrize("n", [1, 5])
+def test_positions_that_the_axes_share_are_refused(n):
+    """An expanded tensor holds one row for all axes; the call would read n per axis."""
+    x = torch.zeros(n, 2, 64)
+    with pytest.raises(api.ConduitError, match="rope_pos"):
+        api.conduit_rotary(x, api.Rope([0.5] * 32, [0, 1] * 16), torch.zeros(1, n, dtype=torch.int32).expand(2, n), x)
