@@ -446,8 +446,8 @@ conduit_status conduit_residual_error(const conduit_kv *kv, const void *q, int32
  * and then to the tensor's dtype.  A factor on cosine and sine (as some context
  * extensions use) belongs into the attention's scale instead.
  * HOST memory, read during the call only (a captured call keeps what it read).
- * A call that turns, appends or loads rows takes up to 2^31 - 4096 heads in all
- * (rows times heads; CONDUIT_ERR_UNSUPPORTED past it).
+ * A call that turns, appends or loads rows takes up to 2^31 - 4096 heads (rows
+ * times heads) and 2^34 dims in all (CONDUIT_ERR_UNSUPPORTED past it).
  * ------------------------------------------------------------------------ */
 #define CONDUIT_MAX_AXES 4
 #define CONDUIT_ROTARY_MAX_DIM 256
@@ -607,7 +607,7 @@ conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, 
  * ws        conduit_attn_mx_workspace_bytes(mx, n, dtype) bytes, 256-byte aligned
  *           (0 bytes: may be NULL).  Needs no initialisation; a captured call
  *           may share it with others that do not run at the same time.
- * Errors: CONDUIT_ERR_UNSUPPORTED if n * n_q_heads exceeds 2^24.
+ * Errors: CONDUIT_ERR_UNSUPPORTED if n * n_q_heads is 2^24 or more.
  * n = 0 enqueues nothing.
  * ------------------------------------------------------------------------ */
 size_t conduit_attn_mx_workspace_bytes(const conduit_kv_mx *mx, int32_t n, int32_t dtype);

@@ -1236,11 +1236,13 @@ conduit_status rope_table(const conduit_rope *rope, const int32_t *rope_pos, int
   return CONDUIT_OK;
 }
 
-// The row kernel numbers all heads of all rows with 31 bits.
-conduit_status check_heads(int32_t n, int64_t heads) {
-  if (n * heads > INT32_MAX - 4095)
-    return fail(CONDUIT_ERR_UNSUPPORTED, "%d rows of %lld heads (supported: up to 2^31 - 4096 heads in all)", n,
-                (long long)heads);
+// The row kernel numbers all heads of all rows with 31 bits, and a launch has
+// fewer than 2^32 threads (up to 1.5 for 8 dims).
+conduit_status check_heads(int32_t n, int64_t heads, int32_t head_dim) {
+  if (n * heads > INT32_MAX - 4095 || n * heads * head_dim > int64_t(1) << 34)
+    return fail(CONDUIT_ERR_UNSUPPORTED,
+                "%d rows of %lld heads of %d dims (supported: up to 2^31 - 4096 heads and 2^34 dims in all)", n,
+                (long long)heads, head_dim);
   return CONDUIT_OK;
 }
 
@@ -1275,7 +1277,7 @@ conduit_status check_new_rows(const conduit_rows *rows, const int32_t *pos, int3
   if (!st && !rows->q != !rows->q_out) st = fail(CONDUIT_ERR_INVALID_ARG, "q and q_out go together");
   if (!st && rows->q) st = check_rows(rows->q, rows->q_stride, q_row, rows->dtype, "rows->q");
   if (!st && rows->q) st = check_rows(rows->q_out, rows->q_out_stride, q_row, rows->dtype, "rows->q_out");
-  if (!st) st = check_heads(rows->n, (int64_t)n_kv_heads + (rows->q ? n_q_heads : 0));
+  if (!st) st = check_heads(rows->n, (int64_t)n_kv_heads + (rows->q ? n_q_heads : 0), head_dim);
   if (!st && rows->q && rows->q == rows->q_out && rows->q_stride != rows->q_out_stride)
     st = fail(CONDUIT_ERR_INVALID_ARG, "q_out in place of q must have its stride");
   if (st) return st;
@@ -1366,7 +1368,7 @@ conduit_status mx_cache(const conduit_kv_mx *mx, int32_t n, MxCache *c) {
   return CONDUIT_OK;
 }
 
-constexpr int64_t kMxMaxPairs = int64_t(1) << 24;
+constexpr int64_t kMxMaxPairs = (int64_t(1) << 24) - 1;  // (a workgroup each: fewer than 2^32 threads)
 
 }  // namespace
 
@@ -1390,7 +1392,7 @@ conduit_status conduit_rotary(const void *x, int64_t x_stride, int32_t n, int32_
   if (!st) st = check_rows(out, out_stride, row, dtype, "out");
   if (!st && x == out && x_stride != out_stride)
     st = fail(CONDUIT_ERR_INVALID_ARG, "out in place of x must have its stride");
-  if (!st) st = check_heads(n, n_heads);
+  if (!st) st = check_heads(n, n_heads, head_dim);
   if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, head_dim, inverse, 2, &rp.rope);
   if (st) return st;
   rp.n = n;
@@ -1460,7 +1462,7 @@ conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, 
   if (n == 0) return ok();
   if (!src_pos || !dst_pos || reinterpret_cast<uintptr_t>(src_pos) % 4 || reinterpret_cast<uintptr_t>(dst_pos) % 4)
     return fail(CONDUIT_ERR_INVALID_ARG, "src_pos and dst_pos must be non-NULL and 4-byte aligned");
-  st = check_heads(n, mx->n_kv_heads);
+  st = check_heads(n, mx->n_kv_heads, mx->head_dim);
   if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, mx->head_dim, 0, 16, &rp.rope);
   if (st) return st;
   rp.n = n;

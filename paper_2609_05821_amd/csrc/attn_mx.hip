@@ -1000,7 +1000,8 @@ MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_head
   // 13 us shared; 2,200 keys 14 and 12 us.  64 sequences of up to 2,048: 15 and 22
   // us.  256 of up to 4,096: 73 and 84 us, of up to 8,192: 142 and 137 us.
   const int64_t from = many || blocks < 256 ? 8 : blocks < 1024 ? 16 : 32;
-  if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX)
+  // (The merge has up to L.pairs workgroups of 256 threads a block, fewer than 2^32.)
+  if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX && blocks * L.pairs < 1 << 24)
     L.n_workers = (int32_t)std::min<int64_t>(resident, std::max<int64_t>(1, blocks * steps / kMinSteps));
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };

@@ -297,3 +297,17 @@ def test_positions_that_the_axes_share_are_refused(n):
     x = torch.zeros(n, 2, 64)
     with pytest.raises(api.ConduitError, match="rope_pos"):
         api.conduit_rotary(x, api.Rope([0.5] * 32, [0, 1] * 16), torch.zeros(1, n, dtype=torch.int32).expand(2, n), x)
+
+
+def test_launch_sizes_end_below_32_bits():
+    """2^32 threads do not fit a launch: refused before, not by it."""
+    n = 1 << 23
+    assert rotary(n=n, heads=32, xs=4096, os_=4096, ps=n) == UNS          # 2^28 heads of 128 dims
+    assert rotary(n=n + 1, heads=256, d=8, xs=2048, os_=2048, ps=n + 1, r=rope(half=4)) == UNS
+    big = mx(n_seqs=1 << 20, n_q_heads=16, n_kv_heads=16, code_stride=16 * 64 * 64, scale_stride=16 * 64 * 4)
+    L = api.lib()
+    assert L.conduit_attn_mx_workspace_bytes(ctypes.byref(big), 1 << 20, api.BF16) == 0
+    assert L.conduit_attn_mx(ctypes.byref(big), FAKE, api.BF16, FAKE, 1 << 20, 0.1, FAKE, None, None, 0, None) == UNS
+    # many blocks of 32 pairs: a workgroup per block, no merge of more than 2^24 pairs
+    wide = mx(n_seqs=2047, n_q_heads=240 * 33, n_kv_heads=240, head_dim=64, n_ctx=1024 * 1024, table_stride=16384)
+    assert L.conduit_attn_mx_workspace_bytes(ctypes.byref(wide), 2047, api.F32) == 0
