@@ -519,6 +519,12 @@ def _one_device(*tensors) -> int:
     return -1 if dev is None else dev
 
 
+def _pool(mx: KVMX) -> Optional[torch.Tensor]:
+    """A tensor of the descriptor's cache, where mx_desc made it."""
+    tensors = getattr(mx, "tensors", None)
+    return tensors[0] if tensors else None
+
+
 def _call(fn, tensors, stream, *args) -> None:
     """fn(*args, stream) with the tensors' device current: one device for all, the
     current stream of that device unless one is given."""
@@ -624,8 +630,9 @@ def conduit_append_mx(mx: KVMX, pos: torch.Tensor, k_new: torch.Tensor, v_new: t
         if t is not None and (t.shape != k_new.shape or t.dtype != k_new.dtype or not t.is_contiguous()):
             raise ConduitError(ERR_INVALID_ARG, "k_out and v_out must be dense and shaped like k_new")
     desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
-    _call(lib().conduit_append_mx, (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), rope_pos),
-          stream, ctypes.byref(mx), ctypes.byref(rows), _ptr(pos), desc, rp, ps, _ptr(k_out), _ptr(v_out))
+    _call(lib().conduit_append_mx,
+          (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), rope_pos, _pool(mx)), stream,
+          ctypes.byref(mx), ctypes.byref(rows), _ptr(pos), desc, rp, ps, _ptr(k_out), _ptr(v_out))
 
 
 def conduit_load_mx(mx: KVMX, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tensor, rope: Optional[Rope] = None,
@@ -634,8 +641,8 @@ def conduit_load_mx(mx: KVMX, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tens
     move (rope_pos [n_axes, n]); see conduit_load_mx."""
     n = src_pos.numel()
     desc, rp, ps = _rope_args(rope, rope_pos, n)
-    _call(lib().conduit_load_mx, (_row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos"), rope_pos), stream,
-          ctypes.byref(mx), _ptr(src_pos), n, ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
+    ids = _row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos")
+    _call(lib().conduit_load_mx, (*ids, rope_pos, _pool(mx)), stream, ctypes.byref(mx), _ptr(src_pos), n, ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
 
 
 def attn_mx_workspace_bytes(mx: KVMX, q: torch.Tensor) -> int:
@@ -662,8 +669,8 @@ def conduit_attn_mx(mx: KVMX, q: torch.Tensor, pos: torch.Tensor, o_out: torch.T
             ws = torch.empty(need, dtype=torch.uint8, device=q.device)
             if stream is not None:
                 ws.record_stream(stream)  # freed on return, used on that stream
-    _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws), stream, ctypes.byref(mx), _ptr(q),
-          _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
+    _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws, _pool(mx)), stream, ctypes.byref(mx),
+          _ptr(q), _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
 
 
 def profile_enable(enabled: bool) -> None:

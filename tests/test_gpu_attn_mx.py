@@ -367,3 +367,16 @@ def test_two_streams():
     torch.cuda.synchronize()
     for (o, l), (wo, wl) in zip(outs, want):
         assert torch.equal(o.cpu(), wo) and torch.equal(l.cpu(), wl)
+
+
+def test_a_pool_on_another_device_is_refused():
+    st = Store(1, 64, 4, 2, 128)
+    cpu = api.mx_desc(*st.cpu, 4, 64, None)
+    x = torch.zeros(2, 4, 128, dtype=torch.bfloat16, device=DEV)
+    kv, pos = x[:, :2], torch.zeros(2, dtype=torch.int32, device=DEV)
+    cache = torch.zeros(64, 2, 128, dtype=torch.bfloat16, device=DEV)
+    for call in (lambda: api.conduit_attn_mx(cpu, x, pos, x.clone()),
+                 lambda: api.conduit_append_mx(cpu, pos, kv, kv),
+                 lambda: api.conduit_load_mx(cpu, pos, api.kv_desc(cache, cache, 4), pos)):
+        with pytest.raises(api.ConduitError, match="different devices"):
+            call()
