@@ -642,7 +642,8 @@ def conduit_load_mx(mx: KVMX, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tens
     n = src_pos.numel()
     desc, rp, ps = _rope_args(rope, rope_pos, n)
     ids = _row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos")
-    _call(lib().conduit_load_mx, (*ids, rope_pos, _pool(mx)), stream, ctypes.byref(mx), _ptr(src_pos), n, ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
+    _call(lib().conduit_load_mx, (*ids, rope_pos, _pool(mx)), stream, ctypes.byref(mx), _ptr(src_pos), n,
+          ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
 
 
 def attn_mx_workspace_bytes(mx: KVMX, q: torch.Tensor) -> int:
