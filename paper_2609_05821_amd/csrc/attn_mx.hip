@@ -25,10 +25,10 @@
 // sequences' lengths; a block that ends up in more than one part is merged by
 // a second launch.  Every workgroup derives the list from the positions itself.
 //
-// Measured: 64 sequences of up to 16,384 tokens (28 heads over 4, head_dim 128, 557
-// MB of codes and scales) 107 us and 6 us to merge, 5.2 TB/s of a large copy's 5.2;
-// one of 65,536 tokens 19 us, of 2,048 11 us (two launches and four dependent loads
-// deep: positions, page, codes, the merge).
+// Measured: 62 sequences of up to 32,768 tokens (28 heads over 4, head_dim 128, 562
+// MB in all) 107 us and 6 us to merge, 5.2 TB/s, the rate of a large copy; one of
+// 65,536 tokens 19 us, of 2,048 11 us (two launches and four dependent loads deep:
+// positions, page, codes, the merge).
 #include <algorithm>
 
 #include "mx.h"
