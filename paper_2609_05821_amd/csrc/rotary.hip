@@ -73,11 +73,12 @@ template <typename T>
 struct Raw {
   u32x4 w[sizeof(T) / 2];
 };
+// (fp32: the second four are `gap` elements after the first)
 template <typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T *p) {
+__device__ __forceinline__ Raw<T> load_raw(const T *p, int gap = 4) {
   Raw<T> r;
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ld16(p + 8 * i / (sizeof(T) / 2));
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ld16(p + gap * i);
   return r;
 }
 __device__ __forceinline__ void expand(const Raw<u16> &r, float (&x)[kVec]) {
@@ -101,11 +102,11 @@ __device__ __forceinline__ void st16_stream(void *p, u32x4 v) {
   __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
 }
 template <typename T>
-__device__ __forceinline__ void store_raw(T *p, const Raw<T> &r) {
+__device__ __forceinline__ void store_raw(T *p, const Raw<T> &r, int gap = 4) {
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) st16_stream(p + 8 * i / (sizeof(T) / 2), r.w[i]);
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) st16_stream(p + gap * i, r.w[i]);
 }
-__device__ __forceinline__ void store(u16 *p, const float (&x)[kVec]) {
+__device__ __forceinline__ void store(u16 *p, const float (&x)[kVec], int = 4) {
   u32x4 r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -114,9 +115,9 @@ __device__ __forceinline__ void store(u16 *p, const float (&x)[kVec]) {
   }
   st16_stream(p, r);
 }
-__device__ __forceinline__ void store(float *p, const float (&x)[kVec]) {
+__device__ __forceinline__ void store(float *p, const float (&x)[kVec], int gap = 4) {
   st16_stream(p, __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}));
-  st16_stream(p + 4, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
+  st16_stream(p + gap, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
 }
 __device__ __forceinline__ float rounded(float x, u16) { return bf16_to_f32(f32_to_bf16(x)); }
 __device__ __forceinline__ float rounded(float x, float) { return x; }
@@ -132,16 +133,17 @@ __device__ __forceinline__ float to_f32(double x) {
 }
 
 // The turn, in place.  x[0] holds dims [o, o + 8) of a head, cs the row's cosines
-// and sines.  FULL: x[1] holds their partners, dims [o + half, o + half + 8).
+// and sines.  FULL: x[1] holds their partners, dims [o + half, o + half + 8), and
+// the second four of either may be `gap` dims after the first.
 // Otherwise y holds the partners (halves; dims from 2 half on have none), or the
 // pairs lie side by side in x[0] (adjacent).
 template <bool FULL, int NV>
 __device__ __forceinline__ void turn(float (&x)[NV][kVec], const float (&y)[kVec], int o, int half, bool adjacent,
-                                     const f64x2 *cs) {
+                                     const f64x2 *cs, int gap) {
   if constexpr (FULL) {
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const f64x2 t = cs[o + j];
+      const f64x2 t = cs[o + j % 4 + j / 4 * gap];
       const double a = x[0][j], b = x[1][j];
       x[0][j] = to_f32(__builtin_fma(a, t[0], -(b * t[1])));
       x[1][j] = to_f32(__builtin_fma(b, t[0], a * t[1]));
@@ -246,7 +248,12 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = p.rope.half, D = p.head_dim;
   const int lanes = D / (kVec * NV), heads = 64 / lanes;  // lanes of a head, heads of the wave's lanes
-  const int sub = lane / lanes, o = (lane - sub * lanes) * kVec;
+  // fp32, all of a head turning: a lane's 8 dims are 4 and, a quarter of the head on,
+  // 4 more, so that a store writes a head's dims side by side (the turn of 16,384
+  // rows of 16 heads of 80 wrote 110 MB instead of 84 with 8 side by side).
+  constexpr bool kSplit = sizeof(T) == 4 && kFull && (MODE == kRowTurn || MODE == kRowAppend);
+  const int gap = kSplit ? half / 2 : 4;
+  const int sub = lane / lanes, o = (lane - sub * lanes) * (kSplit ? 4 : kVec);
   const int units = p.n_q_heads + p.n_kv_heads;           // query heads, then KV heads, of a row
   const int total = p.n * units;
   const bool adjacent = p.rope.adjacent != 0;
@@ -283,7 +290,7 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
       const T *src =
           static_cast<const T *>(query ? p.q : p.k_new) + c.row * (query ? p.q_stride : p.k_new_stride) + h * D;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) c.x[i] = load_raw<T>(src + dims(i));
+      for (int i = 0; i < NV; ++i) c.x[i] = load_raw<T>(src + dims(i), gap);
       c.y = c.x[0];
       if (partners) c.y = load_raw<T>(src + partner);
       if constexpr (MODE != kRowTurn) {
@@ -291,7 +298,7 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           c.v[i] = c.x[i];
-          if (!query) c.v[i] = load_raw<T>(vsrc + dims(i));
+          if (!query) c.v[i] = load_raw<T>(vsrc + dims(i), gap);
         }
       }
     }
@@ -373,11 +380,11 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
     if constexpr (SHAPE == kSingles)
       turn_single<T>(x[0], o, half, rcs, static_cast<const T *>(p.q) + c.row * p.q_stride + c.unit * D);
     else
-      turn<kFull>(x, y, o, half, adjacent, rcs);
+      turn<kFull>(x, y, o, half, adjacent, rcs, gap);
     if (MODE == kRowTurn || c.unit < p.n_q_heads) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        store(static_cast<T *>(p.q_out) + c.row * p.q_out_stride + c.unit * D + dims(i), x[i]);
+        store(static_cast<T *>(p.q_out) + c.row * p.q_out_stride + c.unit * D + dims(i), x[i], gap);
       continue;
     }
     const int h = c.unit - p.n_q_heads;
@@ -389,10 +396,10 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
               (c.at & ((1 << p.pages.shift) - 1));
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        store(static_cast<T *>(p.k) + row * p.k_stride + h * D + dims(i), x[i]);
+        store(static_cast<T *>(p.k) + row * p.k_stride + h * D + dims(i), x[i], gap);
         T *vd = static_cast<T *>(p.v) + row * p.v_stride + h * D + dims(i);
         if constexpr (MODE == kRowAppend)
-          store_raw(vd, c.v[i]);
+          store_raw(vd, c.v[i], gap);
         else
           store(vd, v[i]);
       }
