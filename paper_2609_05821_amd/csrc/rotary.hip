@@ -11,10 +11,12 @@
 // retire in order (65,536 rows of 4 KV heads packed: in a loop over items, which
 // waited for its own stores, 105 us; without the loop 82 us).  Where all of a head
 // turns in halves, a lane holds both dims of its pairs, so that no partner is
-// loaded a second time (72 us), and a head's codes leave in one piece (70 us, 4.4
-// TB/s; a copy of that size reaches 5.2 TB/s).  16,384 rows of 16 heads of 80 in
-// fp32: 34 us, 4.9 TB/s; 17,024 rows of 36 heads of 128 in bf16: 65 us, 4.8 TB/s;
-// 65,536 rows loaded from 4 bits: 38 us, 4.5 TB/s.
+// loaded a second time (72 us), and a head's codes leave in one piece (70 us).  The
+// vector work beside the loads counts: no checks before the turn, packing from
+// bf16 pairs, divisions of small numbers in fp32 (67 us), and LDS for 6 waves per
+// SIMD instead of 5 (64 us, 4.8 TB/s; a copy of that size reaches 5.2 TB/s).
+// 16,384 rows of 16 heads of 80 in fp32: 31 us, 5.4 TB/s; 17,024 rows of 36 heads
+// of 128 in bf16: 62 us, 5.1 TB/s; 65,536 rows loaded from 4 bits: 33 us, 5.1 TB/s.
 // 64-bit arithmetic fits under the loads (v_fma_f64 issues at the rate of an
 // fp32 one on this chip), and it makes the rounding to 4 bits reproducible: no
 // fp32 error of an angle or a product can move a value over a border between
@@ -34,6 +36,7 @@ constexpr int kWaves = kThreads / 64;
 // 65 us; with few rows 1 keeps more waves busy.
 constexpr int kMany = 2;
 constexpr int64_t kManyFrom = 8192;  // units of work from which on
+constexpr int kDppQuad0011 = 0x50, kDppQuad2233 = 0xFA;  // lane i of four <- that of the four
 constexpr int kDppShl4 = 0x104;  // lane i <- lane i + 4 of its 16
 typedef double f64x2 __attribute__((ext_vector_type(2)));
 
@@ -41,7 +44,9 @@ typedef double f64x2 __attribute__((ext_vector_type(2)));
 // constant, fused multiply-adds), then Taylor series on [-pi/4, pi/4], whose
 // first omitted terms are below 5e-17.
 __device__ __forceinline__ f64x2 cos_sin(double a) {
-  const double k = __builtin_rint(a * 0.63661977236758134308);
+  // (1.5 * 2^52 leaves the integer in the low bits; |a| < 2^41.01)
+  const double shifted = __builtin_fma(a, 0.63661977236758134308, 6755399441055744.0);
+  const double k = shifted - 6755399441055744.0;
   double r = __builtin_fma(-k, 1.57079632679489655800e+00, a);
   r = __builtin_fma(-k, 6.12323399573676603587e-17, r);
   const double z = r * r;
@@ -62,8 +67,7 @@ __device__ __forceinline__ f64x2 cos_sin(double a) {
   c = __builtin_fma(c, z, 1.0 / 24.0);
   c = __builtin_fma(c, z, -0.5);
   c = __builtin_fma(c, z, 1.0);
-  // quadrant: k mod 4 (|k| < 2^41, exact)
-  const int q = (int)(k - 4.0 * __builtin_floor(k * 0.25));
+  const int q = (int)__builtin_bit_cast(uint64_t, shifted) & 3;  // k mod 4
   const double cc = q & 1 ? s : c, ss = q & 1 ? c : s;
   return f64x2{q == 1 || q == 2 ? -cc : cc, q >= 2 ? -ss : ss};
 }
@@ -101,26 +105,49 @@ __device__ __forceinline__ void expand(const Raw<float> &r, float (&x)[kVec]) {
 __device__ __forceinline__ void st16_stream(void *p, u32x4 v) {
   __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
 }
-template <typename T>
-__device__ __forceinline__ void store_raw(T *p, const Raw<T> &r, int gap = 4) {
+// Eight of a lane's elements.  fp32: either store writes 16 bytes of every 32, which
+// reach memory in parts, so where four lanes hold 32 dims side by side (gap 0) they
+// trade first and a store writes 64 bytes side by side (16,384 rows of 16 heads of
+// 80 of which 40 dims turn: 46 us, 36 us so); otherwise the second four go `gap`
+// elements on.
+__device__ __forceinline__ void store_words(u16 *p, const u32x4 (&w)[1], int) { st16_stream(p, w[0]); }
+__device__ __forceinline__ void store_words(float *p, const u32x4 (&w)[2], int gap) {
+  if (gap) {
+    st16_stream(p, w[0]);
+    st16_stream(p + gap, w[1]);
+    return;
+  }
+  const int l = threadIdx.x & 3;
+  u32x4 a, b;
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) st16_stream(p + gap * i, r.w[i]);
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t x = w[0][j], y = w[1][j];
+    const uint32_t xa = dpp_mov<kDppQuad0011>(0u, x), ya = dpp_mov<kDppQuad0011>(0u, y);
+    const uint32_t xb = dpp_mov<kDppQuad2233>(0u, x), yb = dpp_mov<kDppQuad2233>(0u, y);
+    a[j] = l & 1 ? ya : xa;
+    b[j] = l & 1 ? yb : xb;
+  }
+  st16_stream(p - 4 * l, a);
+  st16_stream(p - 4 * l + 16, b);
 }
-__device__ __forceinline__ void store(u16 *p, const float (&x)[kVec], int = 4) {
-  u32x4 r;
+template <typename T>
+__device__ __forceinline__ void store_raw(T *p, const Raw<T> &r, int gap) {
+  store_words(p, r.w, gap);
+}
+__device__ __forceinline__ void store(u16 *p, const float (&x)[kVec], int gap) {
+  u32x4 r[1];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const bf16x2 b = {static_cast<__bf16>(x[2 * j]), static_cast<__bf16>(x[2 * j + 1])};
-    r[j] = __builtin_bit_cast(uint32_t, b);
+    r[0][j] = __builtin_bit_cast(uint32_t, b);
   }
-  st16_stream(p, r);
+  store_words(p, r, gap);
 }
-__device__ __forceinline__ void store(float *p, const float (&x)[kVec], int gap = 4) {
-  st16_stream(p, __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}));
-  st16_stream(p + gap, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
+__device__ __forceinline__ void store(float *p, const float (&x)[kVec], int gap) {
+  const u32x4 r[2] = {__builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}),
+                      __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]})};
+  store_words(p, r, gap);
 }
-__device__ __forceinline__ float rounded(float x, u16) { return bf16_to_f32(f32_to_bf16(x)); }
-__device__ __forceinline__ float rounded(float x, float) { return x; }
 __device__ __forceinline__ float one(const u16 *p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ float one(const float *p) { return *p; }
 
@@ -199,61 +226,124 @@ __device__ __forceinline__ void unpack(uint32_t codes, int scale, float (&x)[kVe
   for (int j = 0; j < 4; ++j) x[2 * j] = (float)r[j][0], x[2 * j + 1] = (float)r[j][1];
 }
 
-// Scale byte of a block of 32 dims, 8 of them in each of 4 consecutive lanes:
-// the smallest s with max|x| <= 1.5 * 2^(s - 125), from the bits of the
-// maximum (its exponent, one more when its mantissa is above 1.5).
-__device__ __forceinline__ int block_scale(const float (&x)[kVec]) {
+// A lane's 8 values of a row to be packed: their bits as fp32 or, in pairs, as bf16.
+__device__ __forceinline__ void pack_bits(const float (&x)[kVec], uint32_t (&w)[4], u16) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bf16x2 b = {static_cast<__bf16>(x[2 * j]), static_cast<__bf16>(x[2 * j + 1])};
+    w[j] = __builtin_bit_cast(uint32_t, b);
+  }
+}
+__device__ __forceinline__ void pack_bits(const float (&x)[kVec], uint32_t (&w)[8], float) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = __builtin_bit_cast(uint32_t, x[j]);
+}
+template <typename T>
+__device__ __forceinline__ void raw_bits(const Raw<T> &r, uint32_t (&w)[2 * sizeof(T)]) {
+#pragma unroll
+  for (int j = 0; j < (int)(2 * sizeof(T)); ++j) w[j] = r.w[j / 4][j % 4];
+}
+
+// Largest magnitude of 32 dims, 8 of them in each of 4 consecutive lanes, as the
+// bits of an fp32 number.
+__device__ __forceinline__ uint32_t largest_bits(const uint32_t (&w)[8]) {
   uint32_t m = 0;
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) m = max(m, __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffffu);
+  for (int j = 0; j < 8; ++j) m = max(m, w[j] & 0x7fffffffu);
   m = max(m, dpp_mov<kDppXor1>(0u, m));
-  m = max(m, dpp_mov<kDppXor2>(0u, m));
+  return max(m, dpp_mov<kDppXor2>(0u, m));
+}
+__device__ __forceinline__ uint32_t largest_bits(const uint32_t (&w)[4]) {
+  uint32_t hi = 0, lo = 0;  // (of both halves the upper is enough with the lower below it)
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    hi = max(hi, w[j] & 0x7fffffffu);
+    lo = max(lo, w[j] << 16 & 0x7fffffffu);
+  }
+  uint32_t m = max(hi, lo) & 0xffff0000u;
+  m = max(m, dpp_mov<kDppXor1>(0u, m));
+  return max(m, dpp_mov<kDppXor2>(0u, m));
+}
+
+// Its scale byte: the smallest s with max|x| <= 1.5 * 2^(s - 125) (the maximum's
+// exponent, one more when its mantissa is above 1.5).
+__device__ __forceinline__ int block_scale(uint32_t m) {
   const int s = (int)((m + 0x3fffffu) >> 23) - 2;
   return min(max(s, kMxScaleMin), kMxScaleMax);
 }
 
-__device__ __forceinline__ uint32_t pack(const float (&x)[kVec], int scale) {
+__device__ __forceinline__ uint32_t pack(const uint32_t (&w)[8], int scale) {
   const float s = __builtin_bit_cast(float, (uint32_t)scale << 23);
+  float x[kVec];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t y = w[j];
+    x[j] = __builtin_bit_cast(float, y);
+  }
   uint32_t r = 0;
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[0], x[1], s, 0);
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[2], x[3], s, 1);
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[4], x[5], s, 2);
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6], x[7], s, 3);
 }
-
-__device__ __forceinline__ bool any_not_finite(const float (&x)[kVec]) {
-  uint32_t m = 0;
+__device__ __forceinline__ uint32_t pack(const uint32_t (&w)[4], int scale) {
+  const float s = __builtin_bit_cast(float, (uint32_t)scale << 23);
+  bf16x2 x[4];
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) m = max(m, __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffffu);
-  return m >= 0x7f800000u;
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t y = w[j];
+    x[j] = __builtin_bit_cast(bf16x2, y);
+  }
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x[0], s, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x[1], s, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x[2], s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x[3], s, 3);
+}
+
+__device__ __forceinline__ float scalar(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+// x / d for 0 <= x < d + 128, or x < 512 with d <= 128 (inv: about 1 / d).
+__device__ __forceinline__ int small_div(int x, int d, float inv) {
+  return d > 128 ? x >= d : (int)((x + 0.5f) * inv);
 }
 
 // How a head is shared out over lanes.
 enum HeadShape {
   kVectors = 0,  // 8 dims a lane, partners loaded as well where there are any
-  kPairs = 1,    // all of the head turns, halves: 8 dims of each half a lane
+  kPairs = 1,    // all of the head turns, halves, two heads a row or more: 8 dims of each half a lane
   kSingles = 2   // 8 dims a lane, partners one by one: halves that 8 does not divide (kRowTurn only)
 };
 
 // A head's lanes are lanes of one wave, so a call in place reads every partner
 // before it writes (loads of a wave precede its stores).
+// (6 waves per SIMD, where the compiler would use 2 registers too many for them:
+// 17,024 rows of 36 heads of which 64 dims turn, 78 us, 76 us so.)
 template <typename T, RowMode MODE, int K, HeadShape SHAPE>
-__global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParams p) {
+__global__ __launch_bounds__(kThreads, K == 1                                                         ? 4
+                                       : MODE == kRowAppend && SHAPE == kVectors && sizeof(T) == 2 ? 6
+                                                                                                   : 1)
+void rows_kernel(RowParams p) {
   constexpr bool kToKv = MODE == kRowAppend || MODE == kRowLoadMx, kMx = MODE == kRowAppendMx || MODE == kRowLoadMx;
   constexpr bool kFull = SHAPE == kPairs;
   constexpr int NV = kFull ? 2 : 1;  // vectors of 8 dims of a lane
-  // K = 1: at most 64 / lanes rows of 4 * NV * lanes frequencies each; K > 1 (a
-  // row has that many heads and more): two rows of up to 128.
-  __shared__ f64x2 s_cs[kWaves][256 * NV];
+  // K = 1: at most 64 / lanes rows of 4 * NV * lanes frequencies each, with two heads
+  // a row and more (kPairs) half as many and one; K > 1: two rows of up to 128.
+  // (24 KB at most, which 6 workgroups of a CU fit; with 32 KB and 5 of them 65,536
+  // rows packed took 67 us instead of 64.)
+  __shared__ f64x2 s_cs[kWaves][K == 1 && kFull ? 384 : 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = p.rope.half, D = p.head_dim;
   const int lanes = D / (kVec * NV), heads = 64 / lanes;  // lanes of a head, heads of the wave's lanes
   // fp32, all of a head turning: a lane's 8 dims are 4 and, a quarter of the head on,
   // 4 more, so that a store writes a head's dims side by side (the turn of 16,384
-  // rows of 16 heads of 80 wrote 110 MB instead of 84 with 8 side by side).
+  // rows of 16 heads of 80 wrote 110 MB instead of 84 with 8 side by side: 34.1 and
+  // 31.4 us).
   constexpr bool kSplit = sizeof(T) == 4 && kFull && (MODE == kRowTurn || MODE == kRowAppend);
-  const int gap = kSplit ? half / 2 : 4;
-  const int sub = lane / lanes, o = (lane - sub * lanes) * (kSplit ? 4 : kVec);
+  const int gap = kSplit ? half / 2 : 4, store_gap = kSplit ? gap : lanes % 4 ? 4 : 0;
+  const int sub = (int)((lane + 0.5f) * __builtin_amdgcn_rcpf((float)lanes));
+  const int o = (lane - sub * lanes) * (kSplit ? 4 : kVec);
   const int units = p.n_q_heads + p.n_kv_heads;           // query heads, then KV heads, of a row
   const int total = p.n * units;
   const bool adjacent = p.rope.adjacent != 0;
@@ -263,7 +353,11 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
   f64x2 *cs = s_cs[wave];
   const int first = (blockIdx.x * kWaves + wave) * (heads * K);  // heads of this wave: [first, first + heads * K)
   if (first >= total) return;
-  const int row0 = first / units, row1 = (min(first + heads * K, total) - 1) / units;
+  const int row0 = (int)((uint32_t)first / (uint32_t)units), unit0 = first - row0 * units;
+  const float inv_units = scalar(__builtin_amdgcn_rcpf((float)units));
+  auto row_of = [&](int i) __attribute__((always_inline)) { return small_div(unit0 + i, units, inv_units); };
+  const int last = min(heads * K, total - first) - 1;    // of this wave's heads
+  const int rows = __builtin_amdgcn_readfirstlane(row_of(last)) + 1;
 
   struct In {
     int32_t row, unit;         // of the lane
@@ -277,9 +371,9 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     In &c = in[k];
-    const int u = min(first + k * heads + min(sub, heads - 1), total - 1);  // (past the end: loads the last head)
-    c.row = u / units;
-    c.unit = u - c.row * units;
+    const int u = min(k * heads + min(sub, heads - 1), last), r = row_of(u);  // (past the end: loads the last head)
+    c.row = row0 + r;
+    c.unit = unit0 + u - r * units;
     if constexpr (MODE != kRowTurn) {
       c.at = c.from = p.pos[c.row];
       if constexpr (MODE == kRowLoadMx) c.from = p.src_pos[c.row];
@@ -335,9 +429,10 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
     }
   }
   // The rows' angles.
-  const int n_angles = (row1 - row0 + 1) * half;
+  const int n_angles = rows * half;
+  const float inv_half = scalar(__builtin_amdgcn_rcpf((float)half));
   for (int e = lane; e < n_angles; e += 64) {
-    const int r = e / half, f = e - r * half;
+    const int r = (int)((e + 0.5f) * inv_half), f = e - r * half;
     // (the positions on all axes, so that none waits for the frequency's axis)
     const int32_t *pos = p.rope.pos + row0 + r;
     int32_t at[4];
@@ -357,7 +452,7 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const In &c = in[k];
-    if (sub >= heads || first + k * heads + sub >= total) return;
+    if (sub >= heads || k * heads + sub > last) return;
     const f64x2 *rcs = cs + (c.row - row0) * half;
     float x[NV][kVec], y[kVec], v[NV][kVec];
     if constexpr (MODE == kRowLoadMx) {
@@ -372,11 +467,6 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
       for (int i = 0; i < NV; ++i) expand(c.x[i], x[i]);
       expand(c.y, y);
     }
-    bool bad = false;  // an infinity or a NaN
-    if constexpr (MODE == kRowAppendMx) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) bad = bad || any_not_finite(x[i]);
-    }
     if constexpr (SHAPE == kSingles)
       turn_single<T>(x[0], o, half, rcs, static_cast<const T *>(p.q) + c.row * p.q_stride + c.unit * D);
     else
@@ -384,7 +474,7 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
     if (MODE == kRowTurn || c.unit < p.n_q_heads) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        store(static_cast<T *>(p.q_out) + c.row * p.q_out_stride + c.unit * D + dims(i), x[i], gap);
+        store(static_cast<T *>(p.q_out) + c.row * p.q_out_stride + c.unit * D + dims(i), x[i], store_gap);
       continue;
     }
     const int h = c.unit - p.n_q_heads;
@@ -396,30 +486,32 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
               (c.at & ((1 << p.pages.shift) - 1));
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        store(static_cast<T *>(p.k) + row * p.k_stride + h * D + dims(i), x[i], gap);
+        store(static_cast<T *>(p.k) + row * p.k_stride + h * D + dims(i), x[i], store_gap);
         T *vd = static_cast<T *>(p.v) + row * p.v_stride + h * D + dims(i);
         if constexpr (MODE == kRowAppend)
-          store_raw(vd, c.v[i], gap);
+          store_raw(vd, c.v[i], store_gap);
         else
-          store(vd, v[i]);
+          store(vd, v[i], store_gap);
       }
     }
     if constexpr (MODE == kRowAppendMx) {
       int ks[NV], vs[NV];
       uint32_t kc[NV], vc[NV];
+      // a head with an infinity or a NaN among its keys or values (no turn makes a
+      // finite pair of one that is not): the key is NaN, the value 0
+      bool bad = false;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        expand(c.v[i], v[i]);
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) x[i][j] = rounded(x[i][j], T{});
-        ks[i] = block_scale(x[i]);
-        vs[i] = block_scale(v[i]);
-        kc[i] = pack(x[i], ks[i]);
-        vc[i] = pack(v[i], vs[i]);
-        bad = bad || any_not_finite(x[i]) || any_not_finite(v[i]);
+        uint32_t kw[2 * sizeof(T)], vw[2 * sizeof(T)];
+        pack_bits(x[i], kw, T{});
+        raw_bits<T>(c.v[i], vw);
+        const uint32_t km = largest_bits(kw), vm = largest_bits(vw);
+        ks[i] = block_scale(km);
+        vs[i] = block_scale(vm);
+        kc[i] = pack(kw, ks[i]);
+        vc[i] = pack(vw, vs[i]);
+        bad = bad || max(km, vm) >= 0x7f800000u;
       }
-      // a head with an infinity or a NaN among its keys or values, before or
-      // after the turn: the key is NaN, the value 0
       if (__ballot(bad) >> (sub * lanes) & ((1ull << lanes) - 1)) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -437,11 +529,11 @@ __global__ __launch_bounds__(kThreads, K == 1 ? 4 : 1) void rows_kernel(RowParam
         const int d = dims(i);
         if (p.k_out) {
           unpack(kc[i], ks[i], y);
-          store(static_cast<T *>(p.k_out) + held + d, y);
+          store(static_cast<T *>(p.k_out) + held + d, y, store_gap);
         }
         if (p.v_out) {
           unpack(vc[i], vs[i], y);
-          store(static_cast<T *>(p.v_out) + held + d, y);
+          store(static_cast<T *>(p.v_out) + held + d, y, store_gap);
         }
       }
       if (!c.live) continue;
@@ -488,7 +580,7 @@ void launch_mode(const RowParams &p, RowMode mode, dim3 grid, hipStream_t s) {
       rows_kernel<T, kRowAppend, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
     else if (mode == kRowAppendMx)
       rows_kernel<T, kRowAppendMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
-    else
+    else if constexpr (SHAPE == kVectors || sizeof(T) == 2)
       rows_kernel<T, kRowLoadMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
   }
 }
@@ -509,11 +601,15 @@ hipError_t launch_rows(const RowParams &p, RowMode mode, bool bf16, hipStream_t 
   static const char *const names[] = {"rotary", "append", "append_mx", "load_mx"};
   ProfScope ps(names[mode], s);
   const int half = p.rope.half;
+  const int units = p.n_q_heads + p.n_kv_heads;
+  // (fp32 rows loaded from 4 bits: 8 dims a lane let four lanes trade pieces of one
+  // run of dims instead of two; 65,536 rows 58 us, in pairs 71)
+  const bool pairs = 2 * half == p.head_dim && units > 1 && (bf16 || mode != kRowLoadMx);
   const HeadShape shape = p.rope.adjacent || !half ? kVectors
                           : half % kVec           ? kSingles
-                          : 2 * half == p.head_dim ? kPairs
-                                                   : kVectors;
-  const int heads = 64 / (p.head_dim / (kVec * (shape == kPairs ? 2 : 1))), units = p.n_q_heads + p.n_kv_heads;
+                          : pairs                 ? kPairs
+                                                  : kVectors;
+  const int heads = 64 / (p.head_dim / (kVec * (shape == kPairs ? 2 : 1)));
   const int64_t total = (int64_t)p.n * units;
   const bool many = units >= kMany * heads && total >= kManyFrom * heads;
   const int k = many ? kMany : 1;

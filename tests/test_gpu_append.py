@@ -1,6 +1,8 @@
 """Appends to caches of 16, 32 and 4 bits and loads from the 4-bit cache
 (conduit_append_kv, conduit_append_mx, conduit_load_mx): bit for bit against
 the turn and the packing in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -179,6 +181,31 @@ def test_append_mx_turns_like_the_wide_cache(dtype, d, rot, pairing):
         zero = torch.zeros(n, dtype=torch.long)
         for p, w in zip(pools, (kc, vc, ks, vs)):
             assert torch.equal(M.gather(p.cpu(), table, zero, pos.cpu().long(), page), w)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rot,pairing", [(128, 0), (64, 0), (128, 1)])
+def test_append_mx_turns_no_infinity_into_a_number(dtype, rot, pairing):
+    """Infinities and NaN among keys that turn (by nothing, by a quarter, by any angle)
+    and values: NaN keys, zero values; the other heads as without them."""
+    n, hkv, page, d = 64, 3, 64, 128
+    _, k, v = new_rows(n, hkv, hkv, d, dtype, 4)
+    bad = torch.zeros(n, hkv, dtype=torch.bool)
+    for t, row, h, dim, value in ((k, 0, 0, 0, math.inf), (k, 1, 1, 63, -math.inf), (v, 2, 2, 64, math.nan),
+                                  (k, 3, 0, 127, math.inf), (k, 9, 1, 40, math.inf), (k, 9, 1, 104, math.inf),
+                                  (v, 20, 2, 5, -math.inf), (k, 21, 0, 1, math.nan)):
+        t[row, h, dim] = value
+        bad[row, h] = True
+    inv = np.full(rot // 2, 1.0, np.float32)
+    rope = api.Rope(inv, np.zeros(rot // 2, np.int32), n_axes=1, pairing=pairing)
+    rp = torch.arange(n, dtype=torch.int32, device=DEV)[None].contiguous()
+    rp[0, 3] = 0
+    pools = random_pools(1, hkv, page, d, 5)
+    mx = api.mx_desc(*pools, hkv)
+    api.conduit_append_mx(mx, torch.arange(n, dtype=torch.int32, device=DEV), k, v, rope=rope, rope_pos=rp)
+    kc, vc, ks, vs = (p.cpu()[0].transpose(0, 1) for p in pools)          # [n, hkv, bytes]
+    assert (ks[bad] == 255).all() and (kc[bad] == 0).all() and (vc[bad] == 0).all()
+    assert (ks[~bad] <= 252).all() and (vs <= 252).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -150,3 +150,20 @@ def test_rows_past_32_bits():
     api.conduit_rotary(small, rope, pos, want)
     api.conduit_rotary(x, rope, pos, x)
     assert torch.equal(x.contiguous(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,heads", [(67, 1), (66, 2), (65, 3), (2700, 36)])
+@pytest.mark.parametrize("d,rot,pairing", [(16, 16, 0), (32, 32, 0), (48, 48, 0), (48, 16, 0), (64, 64, 0), (128, 64, 0),
+                                           (128, 128, 1), (176, 176, 0), (256, 256, 0), (256, 20, 0)])
+def test_heads_over_lanes(dtype, n, heads, d, rot, pairing):
+    """Few heads a row and many, over all ways that a head is shared out over lanes."""
+    x = torch.randn(n, heads, d, generator=torch.Generator().manual_seed(d + rot)).to(DT[dtype]).to(DEV)
+    pos = torch.randint(0, 9000, (2, n), generator=torch.Generator().manual_seed(n), dtype=torch.int32).to(DEV)
+    rope = rope_of(rot // 2, 2, pairing)
+    out = torch.full_like(x, 7.0)
+    api.conduit_rotary(x, rope, pos, out)
+    check(out, expect(x, rope, pos), x, DT[dtype])
+    assert torch.equal(out[..., rot:], x[..., rot:])
+    api.conduit_rotary(x, rope, pos, x)
+    assert torch.equal(x, out)
