@@ -32,8 +32,9 @@ constexpr int kThreads = 256;
 constexpr int kVec = 8;  // dims of a lane
 constexpr int kWaves = kThreads / 64;
 // Heads of a wave in units of what its lanes hold, where a row has as many: their
-// angles are shared.  17,024 rows of 36 heads: 1 unit 82 us, 2 units 65 us, 3 units
-// 65 us; with few rows 1 keeps more waves busy.
+// angles are shared.  17,024 rows of 36 heads: 1 unit 67 us, 2 units 62; with 64 of
+// 128 dims that turn 85 and 74; in fp32, whole heads, 107 and 111 us (twice the
+// registers), so 1 there.  With few rows 1 keeps more waves busy.
 constexpr int kMany = 2;
 constexpr int64_t kManyFrom = 8192;  // units of work from which on
 constexpr int kDppQuad0011 = 0x50, kDppQuad2233 = 0xFA;  // lane i of four <- that of the four
@@ -101,7 +102,7 @@ __device__ __forceinline__ void expand(const Raw<float> &r, float (&x)[kVec]) {
 }
 // What is written here is read by another kernel, if at all soon by other XCDs:
 // streaming stores keep it out of the L2's way (65,536 rows loaded from 4 bits:
-// 51 us against 64 us with ordinary stores).
+// 33 us against 49 us with ordinary stores).
 __device__ __forceinline__ void st16_stream(void *p, u32x4 v) {
   __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
 }
@@ -587,12 +588,12 @@ void launch_mode(const RowParams &p, RowMode mode, dim3 grid, hipStream_t s) {
 
 template <typename T, int K>
 void launch_shape(const RowParams &p, RowMode mode, HeadShape shape, dim3 grid, hipStream_t s) {
-  if (shape == kPairs)
-    launch_mode<T, K, kPairs>(p, mode, grid, s);
-  else if (shape == kVectors)
+  if (shape == kVectors)
     launch_mode<T, K, kVectors>(p, mode, grid, s);
-  else
+  else if (shape == kSingles)
     launch_mode<T, K, kSingles>(p, mode, grid, s);
+  else if constexpr (K == 1 || sizeof(T) == 2)
+    launch_mode<T, K, kPairs>(p, mode, grid, s);
 }
 
 }  // namespace
@@ -611,7 +612,7 @@ hipError_t launch_rows(const RowParams &p, RowMode mode, bool bf16, hipStream_t 
                                                   : kVectors;
   const int heads = 64 / (p.head_dim / (kVec * (shape == kPairs ? 2 : 1)));
   const int64_t total = (int64_t)p.n * units;
-  const bool many = units >= kMany * heads && total >= kManyFrom * heads;
+  const bool many = units >= kMany * heads && total >= kManyFrom * heads && (bf16 || shape != kPairs);
   const int k = many ? kMany : 1;
   const dim3 grid((unsigned)((total + heads * k * kWaves - 1) / (heads * k * kWaves)));
   if (bf16)
