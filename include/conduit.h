@@ -591,8 +591,10 @@ conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, 
  * sequence i / (n / n_seqs) (n a multiple of n_seqs) and attends to that
  * sequence's keys 0 .. pos[i].
  *
- * q         device [n][n_q_heads][head_dim] dense, dtype: CONDUIT_BF16, or
- *           CONDUIT_F32 (queries and probabilities then enter the matrix
+ * q         device [n][n_q_heads][head_dim] dense, dtype: CONDUIT_BF16
+ *           (probabilities enter the matrix product in two bf16 parts, up to
+ *           2^-17 of each off; logits, sums and outputs are fp32 and rounded
+ *           once), or CONDUIT_F32 (queries and probabilities enter the matrix
  *           products in three exact bf16 parts, so that nothing is rounded
  *           below fp32).
  * pos       device int32 [n].  Below 0: the row attends to nothing, its output

@@ -16,9 +16,11 @@
 //   O^T += V^T P^T   values are unpacked to bf16 in LDS (each wave its own tile)
 //                and read back with transposing reads; the probabilities are the
 //                other operand as they lie in the S^T accumulators.
-// fp32 queries and probabilities are three exact bf16 parts each; bf16 tensors have
-// their probabilities rounded to bf16 for the product (2^-9 of each, the size of
-// the output's own rounding), while the sum they are divided by stays fp32.
+// fp32 queries and probabilities are three exact bf16 parts each.  With bf16 tensors
+// the probabilities enter the product as two bf16 parts, up to 2^-17 of each off: the
+// output is the 32-bit result but for its own rounding (up to 2^-8), beside which
+// one part (up to 2^-8 of each probability) showed.  The sum that they are divided
+// by is of the fp32 probabilities.
 //
 // The work of a call is the list of all key steps of all (sequence, row block,
 // KV head) blocks.  Workgroups take equal contiguous parts of it, whatever the
@@ -53,7 +55,8 @@ struct Parts {
   bf16x8 v[NS];
 };
 
-// x as the exact sum of NS bf16 parts (NS = 1: rounded).
+// x as the sum of NS bf16 parts, each the nearest to what those before it leave
+// (half a step is up to 2^-8 of a value): three are exact, two up to 2^-17 of x off.
 template <int NS>
 __device__ __forceinline__ void split_parts(const float (&x)[8], Parts<NS> &out) {
   float r[8];
@@ -312,14 +315,15 @@ constexpr int waves_per_simd(int D, int MT, int NS) {
 // rows over 16k tokens: 32 pairs 1,094 us, 16 pairs 823 us).
 constexpr int few_pairs(int D, int64_t pairs, bool bf16) { return pairs <= 16 || (D == 128 && !bf16) ? 16 : 32; }
 
-// MT: groups of 16 pairs of a block.  NS: exact bf16 parts of queries and
-// probabilities (1: bf16 tensors, 3: fp32).  W: waves of a workgroup, 4, or 8 for a
+// MT: groups of 16 pairs of a block.  NS: exact bf16 parts of queries (1: bf16
+// tensors, 3: fp32).  W: waves of a workgroup, 4, or 8 for a
 // workgroup per block on up to 256 blocks (64 sequences of 2,048 keys: 4 waves 20
 // us, 8 waves 15 us; 256 of 512, which leave the CUs several blocks each: 16 and 25 us).
 template <int D, int MT, int NS, int W>
 __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_kernel(MxAttnParams p) {
   constexpr int kWaves = W, kStep = W * kWaveKeys;
   constexpr int kPairs = 16 * MT;
+  constexpr int NP = NS == 1 ? 2 : 3;  // bf16 parts of probabilities
   constexpr int C = D / 32;            // MFMA steps over the dims
   constexpr int DT = D / 16;           // 16-dim tiles of O^T
   constexpr int VP = D + 16;           // value row pitch: 8 rows of a transposing read cover the 64 banks once
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
         }
       }
       wave_lds_fence();
-      Parts<NS> pr[MT];
+      Parts<NP> pr[MT];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         float x[8];
@@ -472,7 +476,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
           x[i] = fast_exp2(x[i] - m[mt]);
           l[mt] += x[i];
         }
-        split_parts<NS>(x, pr[mt]);
+        split_parts<NP>(x, pr[mt]);
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -483,7 +487,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int x = 0; x < NS; ++x)
+          for (int x = 0; x < NP; ++x)
             o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, pr[mt].v[x], o[mt][dt], 0, 0, 0);
       }
       wave_lds_fence();
@@ -742,20 +746,27 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) v0[dt] = v_operand_il<VP>(at + 32 * dt);
       const f32x16 sn = products(nx);
-      bf16x8 pr[2];
+      Parts<2> pr[2];  // of 16 keys each
       float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = fast_exp2(__builtin_fmaf(x.s[i], p.scale_log2, -m));
-        sum[i & 1] += e;
-        pr[i >> 3][i & 7] = static_cast<__bf16>(e);
+      for (int i = 0; i < 2; ++i) {
+        float e[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          e[y] = fast_exp2(__builtin_fmaf(x.s[8 * i + y], p.scale_log2, -m));
+          sum[y & 1] += e[y];
+        }
+        split_parts<2>(e, pr[i]);
       }
       l += sum[0] + sum[1];
+      auto add = [&](int dt, const bf16x8 &v, const Parts<2> &w) __attribute__((always_inline)) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[dt], pr[0], o[dt], 0, 0, 0);
+        for (int y = 0; y < 2; ++y) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w.v[y], o[dt], 0, 0, 0);
+      };
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand_il<VP>(at + 16 * VP + 32 * dt), pr[1], o[dt], 0, 0, 0);
+      for (int dt = 0; dt < DT; ++dt) add(dt, v0[dt], pr[0]);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) add(dt, v_operand_il<VP>(at + 16 * VP + 32 * dt), pr[1]);
       x.s = sn;
       x.top = largest(sn);
       extra();
