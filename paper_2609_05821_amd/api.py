@@ -255,6 +255,15 @@ def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]) -> Optional[torc
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+def _scratch(nbytes: int, device, stream=None) -> torch.Tensor:
+    """Memory for one call on `stream` (None: the current one), from that stream's pool:
+    a block of another stream's may still be in use there."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _nbytes(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
@@ -667,9 +676,7 @@ def conduit_attn_mx(mx: KVMX, q: torch.Tensor, pos: torch.Tensor, o_out: torch.T
     if ws is None:
         need = attn_mx_workspace_bytes(mx, q)
         if need:
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-            if stream is not None:
-                ws.record_stream(stream)  # freed on return, used on that stream
+            ws = _scratch(need, q.device, stream)
     _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws, _pool(mx)), stream, ctypes.byref(mx),
           _ptr(q), _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
 
