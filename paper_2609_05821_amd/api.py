@@ -247,12 +247,12 @@ class ImageTable:
         return int(self.desc.n_images)
 
 
-def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+def _workspace(nbytes: int, device, ws: Optional[torch.Tensor], stream=None) -> Optional[torch.Tensor]:
     if nbytes == 0:
         return ws
     if ws is not None and ws.numel() * ws.element_size() >= nbytes:
         return ws
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _scratch(nbytes, device, stream)
 
 
 def _scratch(nbytes: int, device, stream=None) -> torch.Tensor:
@@ -291,7 +291,7 @@ def conduit_score(kv: KV, q: torch.Tensor, q_pos0: int, img: ImageTable, s_acc: 
     n_q = q.shape[0]
     if scale is None:
         scale = 1.0 / math.sqrt(kv.head_dim)
-    ws = _workspace(score_workspace_bytes(kv, n_q, img), q.device, ws)
+    ws = _workspace(score_workspace_bytes(kv, n_q, img), q.device, ws, stream)
     _check(lib().conduit_score(ctypes.byref(kv), q.data_ptr(), n_q, q_pos0, ctypes.byref(img.desc),
                                norm, agg, scale, _ptr(row_lse_in), _ptr(row_lse_out), _ptr(vnorm_in),
                                s_acc.data_ptr(), a_acc.data_ptr(), int(accumulate), _ptr(a_out),
@@ -310,7 +310,7 @@ def conduit_score_layers(kvs, qs, q_pos0: int, img: "ImageTable", s_acc: torch.T
     n, n_q = len(kvs), qs[0].shape[0]
     if scale is None:
         scale = 1.0 / math.sqrt(kvs[0].head_dim)
-    ws = _workspace(score_layers_workspace_bytes(kvs[0], n_q, img, n), qs[0].device, ws)
+    ws = _workspace(score_layers_workspace_bytes(kvs[0], n_q, img, n), qs[0].device, ws, stream)
     arr = (KV * n)(*kvs)
     vn = None if vnorm_in is None else _ptr_array(vnorm_in)
     _check(lib().conduit_score_layers(arr, n, _ptr_array(qs), n_q, q_pos0, ctypes.byref(img.desc), norm, agg,
@@ -360,7 +360,7 @@ def conduit_residual_error(kv: KV, q: torch.Tensor, q_pos0: int, img: ImageTable
         scale = 1.0 / math.sqrt(kv.head_dim)
     need = residual_workspace_bytes(kv, n_q, img, n_samples, z is not None)
     if ws is None:
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        ws = _scratch(max(need, 1), q.device, stream)
     _check(lib().conduit_residual_error(ctypes.byref(kv), q.data_ptr(), n_q, q_pos0, ctypes.byref(img.desc),
                                         scale, row_lse.data_ptr(), refreshed.data_ptr(), _ptr(z), n_samples,
                                         kappa, err_out.data_ptr(), ws.data_ptr(), ws.numel(),
@@ -376,7 +376,7 @@ def conduit_select_topk(s_acc: torch.Tensor, a_acc: torch.Tensor, n_layers: int,
                         quota_out: Optional[torch.Tensor] = None) -> None:
     """Reweighting and top-k (Eq. 8-11, or a variant rule); see conduit_select_topk."""
     need = int(lib().conduit_select_workspace_bytes(img.n_vis, img.n_images))
-    ws = _workspace(need, s_acc.device, ws)
+    ws = _workspace(need, s_acc.device, ws, stream)
     _check(lib().conduit_select_topk(s_acc.data_ptr(), a_acc.data_ptr(), n_layers,
                                      ctypes.byref(img.desc), lam, rule, k, _ptr(idx_out),
                                      _ptr(pos_out), _ptr(mask_out), _ptr(shat_out), _ptr(c_out),
@@ -418,7 +418,7 @@ def conduit_refresh_attn_layers(kvs, q_sel, pos: torch.Tensor, o_out, lse_out=No
     k, n = pos.numel(), len(kvs)
     if scale is None:
         scale = 1.0 / math.sqrt(kvs[0].head_dim)
-    ws = _workspace(refresh_layers_workspace_bytes(kvs[0], k, n), q_sel[0].device, ws)
+    ws = _workspace(refresh_layers_workspace_bytes(kvs[0], k, n), q_sel[0].device, ws, stream)
     arr = (KV * n)(*kvs)
     lse = None if lse_out is None else ctypes.cast(_ptr_array(lse_out), ctypes.POINTER(ctypes.c_void_p))
     _check(lib().conduit_refresh_attn_layers(arr, n, _ptr_array(q_sel), pos.data_ptr(), k, scale,
@@ -432,7 +432,7 @@ def conduit_refresh_attn(kv: KV, q_sel: torch.Tensor, pos: torch.Tensor, o_out: 
     k = pos.numel()
     if scale is None:
         scale = 1.0 / math.sqrt(kv.head_dim)
-    ws = _workspace(refresh_workspace_bytes(kv, k), q_sel.device, ws)
+    ws = _workspace(refresh_workspace_bytes(kv, k), q_sel.device, ws, stream)
     _check(lib().conduit_refresh_attn(ctypes.byref(kv), q_sel.data_ptr(), pos.data_ptr(), k,
                                       scale, o_out.data_ptr(), _ptr(lse_out), _ptr(ws), _nbytes(ws),
                                       _stream(stream)))
@@ -447,7 +447,7 @@ def conduit_merge_refresh_attn(kv: KV, pos: torch.Tensor, k_new: torch.Tensor, v
     k = pos.numel()
     if scale is None:
         scale = 1.0 / math.sqrt(kv.head_dim)
-    ws = _workspace(refresh_workspace_bytes(kv, k), q_sel.device, ws)
+    ws = _workspace(refresh_workspace_bytes(kv, k), q_sel.device, ws, stream)
     _check(lib().conduit_merge_refresh_attn(ctypes.byref(kv), pos.data_ptr(), k, k_new.data_ptr(), v_new.data_ptr(),
                                             q_sel.data_ptr(), scale, o_out.data_ptr(), _ptr(lse_out), _ptr(ws),
                                             _nbytes(ws), _stream(stream)))
