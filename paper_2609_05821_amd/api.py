@@ -204,8 +204,10 @@ def kv_desc(k: torch.Tensor, v: torch.Tensor, n_q_heads: int) -> KV:
     if k.shape != v.shape or k.dtype != v.dtype:
         raise ConduitError(ERR_INVALID_ARG, "k and v must match in shape and dtype")
     n_ctx, hkv, d = k.shape
-    return KV(k.data_ptr(), v.data_ptr(), k.stride(0), v.stride(0), n_ctx, n_q_heads, hkv, d,
+    desc = KV(k.data_ptr(), v.data_ptr(), k.stride(0), v.stride(0), n_ctx, n_q_heads, hkv, d,
               _dtype_code(k), 0, None, 0)
+    desc.tensors = (k, v)  # kept alive with the descriptor
+    return desc
 
 
 def kv_desc_paged(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,
@@ -224,8 +226,10 @@ def kv_desc_paged(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: tor
     if block_table.dtype != torch.int32 or block_table.dim() != 1 or \
             block_table.numel() < -(-n_ctx // page):
         raise ConduitError(ERR_INVALID_ARG, "block_table must be int32 with ceil(n_ctx / page) entries")
-    return KV(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(1), v_pages.stride(1), n_ctx,
+    desc = KV(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(1), v_pages.stride(1), n_ctx,
               n_q_heads, hkv, d, _dtype_code(k_pages), page, block_table.data_ptr(), n_pages)
+    desc.tensors = (k_pages, v_pages, block_table)  # kept alive with the descriptor
+    return desc
 
 
 class ImageTable:
@@ -528,10 +532,9 @@ def _one_device(*tensors) -> int:
     return -1 if dev is None else dev
 
 
-def _pool(mx: KVMX) -> Optional[torch.Tensor]:
-    """A tensor of the descriptor's cache, where mx_desc made it."""
-    tensors = getattr(mx, "tensors", None)
-    return tensors[0] if tensors else None
+def _held(desc) -> tuple:
+    """The tensors of a descriptor's cache, where mx_desc, kv_desc or kv_desc_paged made it."""
+    return getattr(desc, "tensors", ())
 
 
 def _call(fn, tensors, stream, *args) -> None:
@@ -622,7 +625,7 @@ def conduit_append_kv(kv: KV, pos: torch.Tensor, k_new: torch.Tensor, v_new: tor
     row stride; pos int32 [n], outside the cache: the row is left out."""
     rows = _new_rows(k_new, v_new, q, q_out, kv.n_q_heads, kv.n_kv_heads, kv.head_dim)
     desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
-    _call(lib().conduit_append_kv, (k_new, v_new, q, q_out, _row_ids(pos, rows.n, "pos"), rope_pos), stream,
+    _call(lib().conduit_append_kv, (k_new, v_new, q, q_out, _row_ids(pos, rows.n, "pos"), rope_pos, *_held(kv)), stream,
           ctypes.byref(kv), ctypes.byref(rows), _ptr(pos), desc, rp, ps)
 
 
@@ -640,7 +643,7 @@ def conduit_append_mx(mx: KVMX, pos: torch.Tensor, k_new: torch.Tensor, v_new: t
             raise ConduitError(ERR_INVALID_ARG, "k_out and v_out must be dense and shaped like k_new")
     desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
     _call(lib().conduit_append_mx,
-          (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), rope_pos, _pool(mx)), stream,
+          (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), rope_pos, *_held(mx)), stream,
           ctypes.byref(mx), ctypes.byref(rows), _ptr(pos), desc, rp, ps, _ptr(k_out), _ptr(v_out))
 
 
@@ -651,7 +654,7 @@ def conduit_load_mx(mx: KVMX, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tens
     n = src_pos.numel()
     desc, rp, ps = _rope_args(rope, rope_pos, n)
     ids = _row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos")
-    _call(lib().conduit_load_mx, (*ids, rope_pos, _pool(mx)), stream, ctypes.byref(mx), _ptr(src_pos), n,
+    _call(lib().conduit_load_mx, (*ids, rope_pos, *_held(mx), *_held(kv)), stream, ctypes.byref(mx), _ptr(src_pos), n,
           ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
 
 
@@ -677,8 +680,8 @@ def conduit_attn_mx(mx: KVMX, q: torch.Tensor, pos: torch.Tensor, o_out: torch.T
         need = attn_mx_workspace_bytes(mx, q)
         if need:
             ws = _scratch(need, q.device, stream)
-    _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws, _pool(mx)), stream, ctypes.byref(mx),
-          _ptr(q), _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
+    _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws, *_held(mx)), stream,
+          ctypes.byref(mx), _ptr(q), _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
 
 
 def profile_enable(enabled: bool) -> None:
