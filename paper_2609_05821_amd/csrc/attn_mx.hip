@@ -48,7 +48,21 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kWaveKeys = 32;
 constexpr int kStep = kWaves * kWaveKeys;  // keys of a workgroup step
-constexpr int kMaxSeqBlocks = 4096;        // sequence blocks whose prefix sums fit LDS
+
+// Many pairs per KV head: keys of a tile, pairs of a block, and LDS of a workgroup.
+constexpr int kTileKeys = 64;
+constexpr int kManyPairs = 32 * kWaves;
+constexpr int many_lds(int D) { return 4 * kTileKeys * (D + 16) * 2 + kWaves * 4; }
+
+// Sequence blocks whose list workgroups hold in LDS beside what else they have there:
+// with many pairs as many as leave two workgroups a CU.  (Heads of 128, a list that
+// leaves one, and a workgroup per block instead: 2,060 sequences of 1,024 to 4,096 keys with 5
+// rows, 28 heads over 4, 2,286 and 1,632 us; 60,000 rows of 7 heads over their 60,000 keys 10.4 and
+// 9.2 ms.)
+constexpr int max_seq_blocks(int D, bool many) {
+  const int fit = (160 * 1024 / 2 - many_lds(D)) / 4 - 1;
+  return many && fit < 4096 ? fit : 4096;
+}
 
 template <int NS>
 struct Parts {
@@ -584,8 +598,6 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
 //   each; a pair's column is in two lanes, 16 keys each.
 //   O^T: the probabilities are operands as they lie; the values' rows are stored
 //   interleaved (v_interleaved_key) so that the transposing reads hit every bank once.
-constexpr int kTileKeys = 64;
-constexpr int kManyPairs = 32 * kWaves;
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams p) {
   constexpr int kPairs = kManyPairs;
@@ -596,6 +608,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
   __shared__ __attribute__((aligned(16))) u16 s_v[4][kTileKeys * VP];
   __shared__ int s_sum[kWaves];
   extern __shared__ int s_prefix[];
+  static_assert(sizeof(s_v) + sizeof(s_sum) == many_lds(D), "what max_seq_blocks counts on");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hh = lane >> 5;
   const int hkv = p.mx.n_kv_heads, r = p.mx.rows_per_seq, G = p.group;
@@ -1012,7 +1025,8 @@ MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_head
   // us.  256 of up to 4,096: 73 and 84 us, of up to 8,192: 142 and 137 us.
   const int64_t from = many || blocks < 256 ? 8 : blocks < 1024 ? 16 : 32;
   // (The merge has up to L.pairs workgroups of 256 threads a block, fewer than 2^32.)
-  if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX && blocks * L.pairs < 1 << 24)
+  if (steps > from && n_sb <= max_seq_blocks(head_dim, many) && 2 * blocks * steps < INT32_MAX &&
+      blocks * L.pairs < 1 << 24)
     L.n_workers = (int32_t)std::min<int64_t>(resident, std::max<int64_t>(1, blocks * steps / kMinSteps));
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };

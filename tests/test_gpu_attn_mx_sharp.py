@@ -43,10 +43,11 @@ class Shared:
 
 # (sequences, rows of each, query heads, KV heads, dims, keys): a workgroup of eight and of
 # four waves per block, workgroups that share the steps, 32 pairs a block, many pairs, heads
-# of 64 dims, more blocks than a wave lists, many pairs with as many.
+# of 64 dims, more blocks than a wave lists, many pairs with as many and with more than their
+# lists hold.
 SHAPES = [(30, 1, 8, 2, 128, 1000), (130, 1, 8, 2, 128, 1000), (2, 4, 8, 2, 128, 9000), (12, 3, 14, 2, 128, 1500),
           (1, 700, 7, 1, 128, 4800), (40, 1, 8, 8, 64, 1000), (2, 4, 8, 2, 64, 6000), (1, 500, 8, 2, 64, 4100),
-          (70, 1, 6, 2, 128, 2500), (70, 40, 4, 1, 128, 1100), (70, 40, 4, 1, 64, 1100)]
+          (70, 1, 6, 2, 128, 2500), (70, 40, 4, 1, 128, 1100), (70, 40, 4, 1, 64, 1100), (2060, 5, 7, 1, 128, 1100)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
