@@ -71,7 +71,9 @@ struct Parts {
 
 // x as the sum of NS bf16 parts, each the nearest to what those before it leave
 // (half a step is up to 2^-8 of a value): three are exact, two up to 2^-17 of x off.
-template <int NS>
+// WIDE: the first part is cut off instead (16 of 24 bits are left, which two parts hold),
+// because the largest x would round up to an infinity.
+template <int NS, bool WIDE = false>
 __device__ __forceinline__ void split_parts(const float (&x)[8], Parts<NS> &out) {
   float r[8];
 #pragma unroll
@@ -80,7 +82,11 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], Parts<NS> &out)
   for (int s = 0; s < NS; ++s)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const __bf16 b = static_cast<__bf16>(r[j]);
+      __bf16 b = static_cast<__bf16>(r[j]);
+      if (WIDE && s == 0) {
+        const u16 top = (u16)(__builtin_bit_cast(uint32_t, r[j]) >> 16);
+        b = __builtin_bit_cast(__bf16, top);
+      }
       out.v[s][j] = b;
       if (s + 1 < NS) r[j] -= (float)b;
     }
@@ -411,7 +417,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
             const float *src = static_cast<const float *>(p.q) + at + 8 * c;
             const f32x4 a = __builtin_bit_cast(f32x4, ld16(src)), b = __builtin_bit_cast(f32x4, ld16(src + 4));
             const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-            split_parts<NS>(x, q[mt][c]);
+            split_parts<NS, true>(x, q[mt][c]);
           }
         }
       } else {
