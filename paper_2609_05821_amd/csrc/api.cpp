@@ -1492,7 +1492,8 @@ conduit_status conduit_attn_mx(const conduit_kv_mx *mx, const void *q, int32_t d
   if (!st) st = check_dtype(dtype);
   if (!st) st = mx_cache(mx, n, &ap.mx);
   if (st) return st;
-  if (!(scale > 0.f) || scale == __builtin_inff()) return fail(CONDUIT_ERR_INVALID_ARG, "scale must be finite and > 0");
+  if (!(scale >= 0x1p-126f && scale < 0x1p127f))
+    return fail(CONDUIT_ERR_INVALID_ARG, "scale %g outside [2^-126, 2^127)", scale);
   if ((int64_t)n * mx->n_q_heads > kMxMaxPairs)
     return fail(CONDUIT_ERR_UNSUPPORTED, "n * n_q_heads = %lld exceeds %lld", (long long)n * mx->n_q_heads,
                 (long long)kMxMaxPairs);

@@ -33,3 +33,11 @@ def test_lists_leave_two_workgroups_a_cu(blocks, d):
 @pytest.mark.parametrize("blocks,shared", [(4096, True), (4097, False)])
 def test_lists_of_few_pairs(blocks, shared, dtype):
     assert (workspace(blocks, 1, 8, 128, dtype, ctx=8192) > 0) == shared
+
+
+@pytest.mark.parametrize("scale", [0.0, -1.0, float("nan"), float("inf"), 1e-40, 2.0 ** 127, 3e38])
+def test_scales_that_fp32_cannot_carry(scale):
+    """scale * log2(e), by which the logits are multiplied, has to be a normal number."""
+    mx = api.KVMX(FAKE, FAKE, FAKE, FAKE, 64 * 64, 64 * 4, 1 << 20, 64, 1, 32, 2048, FAKE, 8, 1, 128)
+    st = api.lib().conduit_attn_mx(ctypes.byref(mx), FAKE, api.BF16, FAKE, 3, scale, FAKE, None, FAKE, 1 << 30, None)
+    assert st == api.ERR_INVALID_ARG and "scale" in api.lib().conduit_last_error().decode()
