@@ -28,9 +28,9 @@
 // a second launch.  Every workgroup derives the list from the positions itself.
 //
 // Measured: 62 sequences of up to 32,768 tokens (28 heads over 4, head_dim 128, 562
-// MB in all) 107 us and 6 us to merge, 5.2 TB/s, the rate of a large copy; one of
-// 65,536 tokens 19 us, of 2,048 11 us (two launches and four dependent loads deep:
-// positions, page, codes, the merge).
+// MB in all) 112.5 us and 6.0 us to merge, 5.1 TB/s, about the rate of a large copy (with
+// one part of the probabilities 110.8 us); one of 65,536 tokens 20 us, of 2,048 11 us
+// (two launches and four dependent loads deep: positions, page, codes, the merge).
 #include <algorithm>
 
 #include "mx.h"
@@ -160,7 +160,7 @@ __device__ __forceinline__ int part_begin(int w, int total, int n) { return (int
 // begins there costs a workgroup as much as three steps.  Where parts of up to
 // kOver steps more than equal ones can be cut block by block for the workgroups at
 // hand, they are (`cut`: their length).  8 sequences of up to 8,192 keys with 5 rows
-// 25.1 -> 22.0 us, one of 4,096 with 200 rows 43.4 -> 38.8.
+// 26.0 -> 23.3 us, one of 4,096 with 200 rows 39.5 -> 36.1.
 constexpr int kOver = 2;
 constexpr int kLaneBlocks = 64;
 struct Part {
@@ -332,13 +332,13 @@ constexpr int waves_per_simd(int D, int MT, int NS) {
 }
 // Pairs of a block with few pairs: 32 read the cache once for twice as many, but
 // fp32 rows of 128 dims would leave registers for one wave per SIMD only (1,500
-// rows over 16k tokens: 32 pairs 1,094 us, 16 pairs 823 us).
+// rows over 16k tokens: 32 pairs 1,094 us, 16 pairs 804 us).
 constexpr int few_pairs(int D, int64_t pairs, bool bf16) { return pairs <= 16 || (D == 128 && !bf16) ? 16 : 32; }
 
 // MT: groups of 16 pairs of a block.  NS: exact bf16 parts of queries (1: bf16
 // tensors, 3: fp32).  W: waves of a workgroup, 4, or 8 for a
 // workgroup per block on up to 256 blocks (64 sequences of 2,048 keys: 4 waves 20
-// us, 8 waves 15 us; 256 of 512, which leave the CUs several blocks each: 16 and 25 us).
+// us, 8 waves 16 us; 256 of 512, which leave the CUs several blocks each: 16 and 24 us).
 template <int D, int MT, int NS, int W>
 __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_kernel(MxAttnParams p) {
   constexpr int kWaves = W, kStep = W * kWaveKeys;
@@ -594,12 +594,15 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
 // products and the vector work between them.  The waves of a workgroup take 32
 // pairs each and go over the same keys, 64 at a time.  Keys are unpacked by every
 // wave for itself straight into operands, values once per workgroup into LDS, two
-// tiles ahead.  (1,638 rows of 28 heads over 17,024 keys: 240 us, 833 TFLOP/s, and 14
-// us to merge; matrix cores busy 37% of the cycles, 9 vector instructions a product.
-// Keys through LDS as well, unpacked once for 8 waves: 5% slower, and 13% slower with
-// every product and its vector work in a fixed slot.)  Products are v_mfma_f32_32x32x16_bf16: beside it a wave issues
-// vector instructions for free, beside 16x16x32 it does not (16 of the former with
-// 64 fma between them 543 cycles, 32 of the latter, the same products, 659).
+// tiles ahead.  (1,638 rows of 28 heads over 17,024 keys: 306 us with the 14 that the
+// merge takes, 653 TFLOP/s of the two products' and half as much again for the second
+// part of the probabilities; matrix cores busy 44% of the cycles, 8.6 vector
+// instructions a product.  With one part 246 us; there keys through LDS as well,
+// unpacked once for 8 waves, took 5% more, every product and its vector work in a fixed
+// slot nothing more or less, both together 13% more.)  Products are
+// v_mfma_f32_32x32x16_bf16: beside it a wave issues vector instructions for free, beside
+// 16x16x32 it does not (16 of the former with 64 fma between them 543 cycles, 32 of the
+// latter, the same products, 659).
 //   S^T: lane (key, h) holds half h of the key's dims, codes and scales in one piece
 //   each; a pair's column is in two lanes, 16 keys each.
 //   O^T: the probabilities are operands as they lie; the values' rows are stored
@@ -888,7 +891,7 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int 
   constexpr int kGroups = 256 / L4, kShare = kGroups / PW;
   // Parts a group has on their way at a time: where a workgroup shares one pair's,
   // there may be a hundred (one sequence of 65,536 keys, both launches: one at a
-  // time 23.8 us, four 19.0).
+  // time 23.8 us, four 19.9).
   constexpr int kBatch = PW == 1 ? 4 : 1;
   __shared__ float s_m[kGroups], s_l[kGroups];
   __shared__ f32x4 s_o[kShare > 1 ? kGroups : 1][L4];
@@ -1027,8 +1030,8 @@ MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_head
   // this many steps of a block on (and while the parts' list fits LDS): fewer are
   // done sooner by a workgroup per block, and the more blocks there are the less
   // there is to even out.  One sequence of 4 KV heads: 1,024 keys 9 us by block,
-  // 13 us shared; 2,200 keys 14 and 12 us.  64 sequences of up to 2,048: 15 and 22
-  // us.  256 of up to 4,096: 73 and 84 us, of up to 8,192: 142 and 137 us.
+  // 11 us shared; 2,200 keys 14 and 11 us.  64 sequences of up to 2,048: 15 and 20
+  // us.  256 of up to 4,096: 75 and 84 us, of up to 8,192: 144 and 140 us.
   const int64_t from = many || blocks < 256 ? 8 : blocks < 1024 ? 16 : 32;
   // (The merge has up to L.pairs workgroups of 256 threads a block, fewer than 2^32.)
   if (steps > from && n_sb <= max_seq_blocks(head_dim, many) && 2 * blocks * steps < INT32_MAX &&

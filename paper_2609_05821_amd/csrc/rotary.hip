@@ -14,9 +14,10 @@
 // loaded a second time (72 us), and a head's codes leave in one piece (70 us).  The
 // vector work beside the loads counts: no checks before the turn, packing from
 // bf16 pairs, divisions of small numbers in fp32 (67 us), and LDS for 6 waves per
-// SIMD instead of 5 (64 us, 4.8 TB/s; a copy of that size reaches 5.2 TB/s).
-// 16,384 rows of 16 heads of 80 in fp32: 31 us, 5.4 TB/s; 17,024 rows of 36 heads
-// of 128 in bf16: 62 us, 5.1 TB/s; 65,536 rows loaded from 4 bits: 33 us, 5.1 TB/s.
+// SIMD instead of 5 (64 us; the kernel as it stands 60.6 us, 5.1 TB/s, where a copy
+// of that size reaches 5.2).  16,384 rows of 16 heads of 80 in fp32: 32.2 us, 6.1 TB/s
+// with lines written in two parts; 17,024 rows of 36 heads of 128 in bf16: 59.1 us, 5.3
+// TB/s; 65,536 rows loaded from 4 bits: 31.8 us, 5.7 TB/s.
 // 64-bit arithmetic fits under the loads (v_fma_f64 issues at the rate of an
 // fp32 one on this chip), and it makes the rounding to 4 bits reproducible: no
 // fp32 error of an angle or a product can move a value over a border between
@@ -339,8 +340,8 @@ void rows_kernel(RowParams p) {
   const int lanes = D / (kVec * NV), heads = 64 / lanes;  // lanes of a head, heads of the wave's lanes
   // fp32, all of a head turning: a lane's 8 dims are 4 and, a quarter of the head on,
   // 4 more, so that a store writes a head's dims side by side (the turn of 16,384
-  // rows of 16 heads of 80 wrote 110 MB instead of 84 with 8 side by side: 34.1 and
-  // 31.4 us).
+  // rows of 16 heads of 80 writes 109 MB for its 84, and 130 with 8 side by side: 38.2 and
+  // 41.8 us over four inputs).
   constexpr bool kSplit = sizeof(T) == 4 && kFull && (MODE == kRowTurn || MODE == kRowAppend);
   const int gap = kSplit ? half / 2 : 4, store_gap = kSplit ? gap : lanes % 4 ? 4 : 0;
   const int sub = (int)((lane + 0.5f) * __builtin_amdgcn_rcpf((float)lanes));

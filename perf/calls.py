@@ -3,8 +3,7 @@
     python3 perf/calls.py [NAME,NAME...] [calls of each case] [inputs of each case]
 
 Every case (or those whose names begin so) is prepared from as many seeds as it has inputs and
-called on one after the other; the large cases' inputs together are several times what a
-cache holds.  Prints the time of a call: of the host alone, and with the GPU.
+called on one after the other.  Prints the time of a call: of the host alone, and with the GPU.
 """
 import os
 import sys
