@@ -603,8 +603,9 @@ conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, 
  *           Keys past a row's position do not enter its output, whatever they
  *           hold.
  * scale     from 2^-126 to below 2^127; |scale * q.k| below 2^30 and the sum of
- *           |q_i k_i| below 2^127 for every key that a row attends to (the row is
- *           meaningless otherwise).
+ *           |q_i k_i| below 2^127 for every key that a row attends to, and in every
+ *           dim the sum of |v| over those keys below 2^119 (the row is meaningless
+ *           otherwise).
  * o_out     device [n][n_q_heads][head_dim], dtype.
  * lse_out   nullable device [n][n_q_heads] fp32: natural-log log-sum-exp.
  * ws        conduit_attn_mx_workspace_bytes(mx, n, dtype) bytes, 256-byte aligned
