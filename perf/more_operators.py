@@ -6,12 +6,12 @@ the definitions in 64 bits.  With ``own`` false ``run`` computes the operators
 in elementary torch operations; with ``own`` true it calls the package.  The
 kinds of case:
 
-  append_q8  new (or recomputed) keys and values into a cache held in 8 bits,
-             quantised as they are written, the keys (and the queries of the
-             same tokens) rotated on the way;
-  load_q8    rows of such a cache into a cache of 16 or 32 bits, the keys
-             rotated by the distance that they move;
-  attn_q8    attention over such a cache.
+  append_byte  new (or recomputed) keys and values into a cache held in 8 bits,
+               quantised as they are written, the keys (and the queries of the
+               same tokens) rotated on the way;
+  load_byte    rows of such a cache into a cache of 16 or 32 bits, the keys
+               rotated by the distance that they move;
+  attn_byte    attention over such a cache.
 
 The 8-bit cache: a scale byte s for each block of 16 tokens and head, and codes
 c in e4m3 (sign, 4 exponent bits, 3 mantissa bits, up to 448); the value is
@@ -54,29 +54,29 @@ def listed():
     return [
         # A decoding batch: one token each of 64 sequences of up to 1,024 tokens (two of them padding), handed
         # back as the cache holds them.
-        _case("append_q8", name="append_decode", n_seqs=64, rows=1, ctx=1024, ragged=True, pad=2, held=True),
+        _case("append_byte", name="append_decode", n_seqs=64, rows=1, ctx=1024, ragged=True, pad=2, held=True),
         # A refresh step's rows (10% of 16k visual tokens) written over stale ones: blocks of kept and new tokens.
-        _case("append_q8", name="append_refresh", rows=1638, ctx=17024, spread=True),
+        _case("append_byte", name="append_refresh", rows=1638, ctx=17024, spread=True),
         # A whole 16k multi-image prompt, one layer.
-        _case("append_q8", name="append_prompt", rows=17024, ctx=17024),
+        _case("append_byte", name="append_prompt", rows=17024, ctx=17024),
         # A long document's fp32 keys and values packed for reuse.
-        _case("append_q8", name="append_document_f32", dtype="f32", rows=65536, ctx=65536, with_q=False),
+        _case("append_byte", name="append_document_f32", dtype="f32", rows=65536, ctx=65536, with_q=False),
         # One image of a store loaded into a request's fp32 cache, its keys moved to their new place.
-        _case("load_q8", name="load_image_f32", dtype="f32", rows=1024, ctx=1344),
+        _case("load_byte", name="load_image_f32", dtype="f32", rows=1024, ctx=1344),
         # A long document loaded into a bf16 cache.
-        _case("load_q8", name="load_document", rows=65536, ctx=66048),
+        _case("load_byte", name="load_document", rows=65536, ctx=66048),
         # One token, fp32, one image of context, 8 heads of 64: the smallest attention.
-        _case("attn_q8", name="attn_token_f32", dtype="f32", hq=8, hkv=8, d=64, ctx=672),
+        _case("attn_byte", name="attn_token_f32", dtype="f32", hq=8, hkv=8, d=64, ctx=672),
         # A decoding batch of 64 ragged sequences of up to 32k tokens (two of them padding).
-        _case("attn_q8", name="attn_decode", n_seqs=64, ctx=32768, ragged=True, pad=2),
+        _case("attn_byte", name="attn_decode", n_seqs=64, ctx=32768, ragged=True, pad=2),
         # One token of a single very long sequence.
-        _case("attn_q8", name="attn_long", hq=32, hkv=8, ctx=131072),
+        _case("attn_byte", name="attn_long", hq=32, hkv=8, ctx=131072),
         # Five drafted tokens of each of 8 sequences verified at once, an odd context.
-        _case("attn_q8", name="attn_draft", n_seqs=8, rows=5, hq=32, hkv=8, ctx=8211, ragged=True),
+        _case("attn_byte", name="attn_draft", n_seqs=8, rows=5, hq=32, hkv=8, ctx=8211, ragged=True),
         # Text rows of 4 requests attending to all of an encoder's states, whose number differs by request.
-        _case("attn_q8", name="attn_cross", n_seqs=4, rows=333, hq=32, hkv=8, ctx=4100, ragged=True, cross=True),
+        _case("attn_byte", name="attn_cross", n_seqs=4, rows=333, hq=32, hkv=8, ctx=4100, ragged=True, cross=True),
         # The refresh step's selected rows (10% of 16k visual tokens).
-        _case("attn_q8", name="attn_refresh", rows=1638, ctx=17024, spread=True),
+        _case("attn_byte", name="attn_refresh", rows=1638, ctx=17024, spread=True),
     ]
 
 
@@ -85,7 +85,7 @@ def _log_int(rng, lo, hi):
 
 
 def draw(rng):
-    kind = rng.choice(["append_q8", "append_q8", "load_q8", "attn_q8", "attn_q8", "attn_q8"])
+    kind = rng.choice(["append_byte", "append_byte", "load_byte", "attn_byte", "attn_byte", "attn_byte"])
     dtype = rng.choice(["bf16", "bf16", "f32"])
     d = rng.choice([64, 128, 128])
     hkv = rng.choice([1, 2, 4, 8])
@@ -93,22 +93,22 @@ def draw(rng):
     page = rng.choice([64, 128, 256])
     axes = rng.choice([1, 2, 3, 4])
     pairing = rng.choice([HALVES, HALVES, ADJACENT])
-    if kind != "attn_q8":
-        with_q = kind == "append_q8" and rng.random() < 0.6
+    if kind != "attn_byte":
+        with_q = kind == "append_byte" and rng.random() < 0.6
         per_row = (hq if with_q else 0) + 2 * hkv
         rot = rng.choice([d, d, d // 2])
         spread, n_seqs, how = False, 1, rng.random()
-        if kind == "append_q8" and how < 0.4:            # a decoding batch
+        if kind == "append_byte" and how < 0.4:            # a decoding batch
             n_seqs, rows = _log_int(rng, 2, 256), rng.choice([1, 1, 2, 4])
             ctx = rows + _log_int(rng, 1, 1024)
-        elif kind == "append_q8" and how < 0.6:          # rows recomputed here and there
+        elif kind == "append_byte" and how < 0.6:          # rows recomputed here and there
             ctx = _log_int(rng, 64, 16384)
             rows, spread = _log_int(rng, 1, max(1, ctx // 3)), True
         else:
             rows = _log_int(rng, 1, min(65536, 2 ** 25 // (per_row * d)))
             ctx = rows + _log_int(rng, 1, 1024)
         return _case(kind, dtype=dtype, n_seqs=n_seqs, rows=rows, hq=hq, hkv=hkv, d=d, ctx=ctx, page=page, rot=rot,
-                     axes=axes, pairing=pairing, with_q=with_q, held=kind == "append_q8" and rng.random() < 0.4,
+                     axes=axes, pairing=pairing, with_q=with_q, held=kind == "append_byte" and rng.random() < 0.4,
                      spread=spread, ragged=n_seqs > 1, pad=rng.choice([0, 0, 1]) if n_seqs > 1 else 0)
     how = rng.random()
     if how < 0.35:                                       # rows of one sequence
@@ -213,13 +213,13 @@ def _inputs(case, seed):
     n = case["n_seqs"] * case["rows"]
     table, n_pages = _table(case, rng)
     st = dict(case=case, table=table)
-    if case["kind"] != "attn_q8":
+    if case["kind"] != "attn_byte":
         inv, axis = _frequencies(case)
         st.update(inv=inv, axis=axis, inv_dev=torch.from_numpy(inv).to(DEV),
                   axis_dev=torch.from_numpy(axis.astype(np.int64)).to(DEV))
     st["k8"], st["k8s"] = _random_pool(case, n_pages, gen)
     st["v8"], st["v8s"] = _random_pool(case, n_pages, gen)
-    if case["kind"] == "append_q8":
+    if case["kind"] == "append_byte":
         st["pos"] = _positions(case, rng)
         # the projections' output: queries, keys and values of a token side by side
         width = (hq if case["with_q"] else 0) + 2 * hkv
@@ -233,14 +233,14 @@ def _inputs(case, seed):
         # rows written over others: all of the sequence is there already
         st["n_held"] = (torch.full((case["n_seqs"],), case["ctx"], dtype=torch.int32, device=DEV)
                         if case["spread"] else None)
-    if case["kind"] == "load_q8":
+    if case["kind"] == "load_byte":
         # the first `rows` tokens of the store go to the request's tokens from a shift on
         shift = case["ctx"] - case["rows"]
         st["pos"] = torch.arange(n, dtype=torch.int32, device=DEV)
         st["dst_pos"] = st["pos"] + shift
         st["rope_pos"] = torch.full((case["axes"], n), shift, dtype=torch.int32, device=DEV)
         st["k"], st["v"] = (torch.zeros(case["ctx"], hkv, d, dtype=dt, device=DEV) for _ in range(2))
-    if case["kind"] == "attn_q8":
+    if case["kind"] == "attn_byte":
         st["pos"] = _positions(case, rng)
         st["q"] = _normal(gen, n, hq, d).to(dt)
         st["o"] = torch.empty(n, hq, d, dtype=dt, device=DEV)
@@ -253,14 +253,14 @@ def prepare(case, seed):
     if not own:
         return st
     from paper_2609_05821_amd import api
-    if case["kind"] != "attn_q8":
+    if case["kind"] != "attn_byte":
         st["rope"] = api.Rope(st["inv"], st["axis"], n_axes=case["axes"],
                               pairing=api.PAIR_ADJACENT if case["pairing"] == ADJACENT else api.PAIR_HALVES)
-    if case["kind"] == "load_q8":
+    if case["kind"] == "load_byte":
         st["kv"] = api.kv_desc(st["k"], st["v"], case["hq"])
-    st["q8"] = api.q8_desc(st["k8"], st["v8"], st["k8s"], st["v8s"], case["hq"], case["ctx"], st["table"])
-    if case["kind"] == "attn_q8":
-        need = api.attn_q8_workspace_bytes(st["q8"], st["q"])
+    st["cache"] = api.byte_desc(st["k8"], st["v8"], st["k8s"], st["v8s"], case["hq"], case["ctx"], st["table"])
+    if case["kind"] == "attn_byte":
+        need = api.attn_byte_workspace_bytes(st["cache"], st["q"])
         st["ws"] = torch.empty(max(need, 1), dtype=torch.uint8, device=DEV)
     return st
 
@@ -281,15 +281,15 @@ def _pools(st):
 def _run_own(st):
     from paper_2609_05821_amd import api
     kind = st["case"]["kind"]
-    if kind == "append_q8":
-        api.conduit_append_q8(st["q8"], st["pos"], st["k_new"], st["v_new"], n_held=st["n_held"], rope=st["rope"],
+    if kind == "append_byte":
+        api.conduit_append_byte(st["cache"], st["pos"], st["k_new"], st["v_new"], n_held=st["n_held"], rope=st["rope"],
                               rope_pos=st["rope_pos"], q=st["q"], q_out=st["q_out"], k_out=st["k_held"],
                               v_out=st["v_held"])
         return _pools(st) + [t for t in (st["q_out"], st["k_held"], st["v_held"]) if t is not None]
-    if kind == "load_q8":
-        api.conduit_load_q8(st["q8"], st["pos"], st["kv"], st["dst_pos"], rope=st["rope"], rope_pos=st["rope_pos"])
+    if kind == "load_byte":
+        api.conduit_load_byte(st["cache"], st["pos"], st["kv"], st["dst_pos"], rope=st["rope"], rope_pos=st["rope_pos"])
         return [st["k"], st["v"]]
-    api.conduit_attn_q8(st["q8"], st["q"], st["pos"], st["o"], lse_out=st["lse"], ws=st["ws"])
+    api.conduit_attn_byte(st["cache"], st["q"], st["pos"], st["o"], lse_out=st["lse"], ws=st["ws"])
     return [st["o"], st["lse"]]
 
 
@@ -344,11 +344,11 @@ def _held(codes, scales):
 def _run_plain(st):
     c = st["case"]
     kind = c["kind"]
-    if kind == "attn_q8":
+    if kind == "attn_byte":
         return _plain_attention(st)
     n, page = st["pos"].numel(), c["page"]
     p = st["pos"].long()
-    if kind == "load_q8":
+    if kind == "load_byte":
         at_page, at_slot = st["table"][0, p // page].long(), p % page
         k, v = (_numbers(codes[at_page, :, at_slot]) *
                 _two_to(scales[at_page, :, at_slot // BLOCK].int() - 127)[..., None]
@@ -453,9 +453,9 @@ def _plain_attention(st):
 def exact(case, seed):
     st = _inputs(case, seed)
     page = case["page"]
-    if case["kind"] == "attn_q8":
+    if case["kind"] == "attn_byte":
         return _exact_attention(st)
-    if case["kind"] == "load_q8":
+    if case["kind"] == "load_byte":
         at = [(int(t) // page, int(t) % page) for t in st["pos"].tolist()]
         pg = st["table"][0].long()[torch.tensor([a for a, _ in at], device=DEV)]
         sl = torch.tensor([b for _, b in at], device=DEV)
@@ -605,15 +605,16 @@ def work(case):
     n, live = n_seqs * r, (n_seqs - case["pad"]) * r
     kind = case["kind"]
     ids = 4 * (case["axes"] + 1) * n
-    if kind == "append_q8":
+    if kind == "append_byte":
         q = 2 * n * hq * d * es if case["with_q"] else 0
         q_flops = 3 * n * hq * case["rot"] if case["with_q"] else 0
         held = 2 * n * hkv * d * es if case["held"] else 0
         blocks = live if case["spread"] or r < BLOCK else live / BLOCK
         return {"bytes": int(2 * live * hkv * d * (es + 1) + 2 * blocks * hkv + held + q + ids),
                 "flops": live * hkv * (3 * case["rot"] + 4 * d) + q_flops}
-    if kind == "load_q8":
-        return {"bytes": int(2 * n * hkv * (d + 1 / BLOCK + d * es) + ids), "flops": n * hkv * (3 * case["rot"] + 2 * d)}
+    if kind == "load_byte":
+        return {"bytes": int(2 * n * hkv * (d + 1 / BLOCK + d * es) + ids),
+                "flops": n * hkv * (3 * case["rot"] + 2 * d)}
     lo = 1 if case["cross"] else r
     lengths = [case["ctx"]] * n_seqs
     if case["ragged"]:
