@@ -620,6 +620,87 @@ conduit_status conduit_attn_mx(const conduit_kv_mx *mx, const void *q, int32_t d
                                float scale, void *o_out, float *lse_out, void *ws, size_t ws_bytes,
                                hipStream_t stream);
 
+/* One layer's KV cache in 8 bits, for one or more sequences.
+ *
+ * 16 consecutive tokens of a page (a block) share a scale byte s per head; codes are
+ * e4m3 (sign, 4 exponent bits, 3 mantissa bits; up to 448; 0x7f and 0xff are NaN).  A
+ * value is code * 2^(s - 127), exact in bf16.
+ *
+ * Pools: page p holds [n_kv_heads][page_size][head_dim] code bytes at k + p *
+ * code_stride, and [n_kv_heads][page_size / 16] scale bytes at k_scale + p *
+ * scale_stride; v likewise.  Sequences, pages and the block table are those of
+ * conduit_kv_mx.  Scale bytes outside [10, 246], which no append writes, are read as
+ * the nearest of these. */
+typedef struct {
+  void *k;                /* device code bytes, 16-byte aligned                      */
+  void *v;
+  void *k_scale;          /* device scale bytes, 4-byte aligned                      */
+  void *v_scale;
+  int64_t code_stride;    /* bytes between pages of k and of v: a multiple of 16,
+                             >= n_kv_heads * page_size * head_dim                    */
+  int64_t scale_stride;   /* the same for k_scale and v_scale: a multiple of 4,
+                             >= n_kv_heads * page_size / 16                          */
+  int32_t n_pages;        /* pages in each pool                                      */
+  int32_t page_size;      /* tokens per page: a power of two from 64 to 2^20         */
+  int32_t n_seqs;         /* sequences                                               */
+  int32_t table_stride;   /* pages of a sequence                                     */
+  int32_t n_ctx;          /* tokens a sequence holds: 1 .. table_stride * page_size  */
+  const int32_t *block_table; /* device [n_seqs][table_stride], or NULL              */
+  int32_t n_q_heads;      /* a multiple of n_kv_heads                                */
+  int32_t n_kv_heads;     /* up to 256                                               */
+  int32_t head_dim;       /* 64 or 128                                               */
+} conduit_kv_byte;
+
+/* ------------------------------------------------------------------------ *
+ * conduit_append_kv into an 8-bit cache.  Rows are shared out evenly over the
+ * sequences: row i is token pos[i] of sequence i / (n / n_seqs), and n must be a
+ * multiple of n_seqs.  Rows may be bf16 or fp32.
+ *
+ * The rows that go to one block take, for each head, the smallest s in [10, 246] with
+ * max|x| <= 448 * 2^(s - 127), and the nearest codes, ties to the even code; x is the row
+ * as a cache of rows->dtype would hold it (larger x take the largest code).  Where the
+ * block keeps tokens that the call does not write, s is no less than the block's; where
+ * it rises, the kept codes are rounded to it.  What a block holds thus depends on the
+ * calls that filled it only by this rounding of codes that the new scale makes
+ * subnormal (below 2^-6).  A token that has an infinity or a NaN among its keys or values
+ * of some head has NaN codes in that head's keys and zero values, and counts for no scale:
+ * rows that attend to it are NaN there.
+ *
+ * pos       device int32 [n].  Within a sequence the positions in [0, n_ctx) ascend
+ *           (a block that they come back to has meaningless contents); of rows with one
+ *           position one is held.  A row whose position is outside leaves the cache as
+ *           it was (padded rows: -1); its q_out is still written.
+ * n_held    nullable device int32 [n_seqs]: tokens that each sequence holds before the
+ *           call, 0 .. n_held[s] - 1, are kept (values outside [0, n_ctx] are read as the
+ *           nearest).  NULL, for rows behind all others: what a block has before the last
+ *           row that it receives is kept.  Other tokens of the blocks that rows go to
+ *           are free: their codes stay as they were while the scale may not.
+ * k_out, v_out  nullable device [n][n_kv_heads][head_dim] dense, rows->dtype: the
+ *           keys and values as the cache holds them (a row that pos leaves out: as in a
+ *           block of its own).  May not overlap the rows.
+ * ------------------------------------------------------------------------ */
+conduit_status conduit_append_byte(const conduit_kv_byte *cache, const conduit_rows *rows, const int32_t *pos,
+                                   const int32_t *n_held, const conduit_rope *rope, const int32_t *rope_pos,
+                                   int64_t rope_pos_stride, void *k_out, void *v_out, hipStream_t stream);
+
+/* conduit_load_mx from an 8-bit cache. */
+conduit_status conduit_load_byte(const conduit_kv_byte *cache, const int32_t *src_pos, int32_t n, const conduit_kv *kv,
+                                 const int32_t *dst_pos, const conduit_rope *rope, const int32_t *rope_pos,
+                                 int64_t rope_pos_stride, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * conduit_attn_mx over an 8-bit cache: the same rows, arguments, limits and results.  With
+ * every row's position at its sequence's last token this is attention to all of it, for
+ * example of a text's rows to an encoder's states of another length.  Among the values of
+ * tokens that a row does not see NaN codes are harmless; among those that it sees they
+ * count as NaN or as 0 (appends write none).
+ * ------------------------------------------------------------------------ */
+size_t conduit_attn_byte_workspace_bytes(const conduit_kv_byte *cache, int32_t n, int32_t dtype);
+
+conduit_status conduit_attn_byte(const conduit_kv_byte *cache, const void *q, int32_t dtype, const int32_t *pos,
+                                 int32_t n, float scale, void *o_out, float *lse_out, void *ws, size_t ws_bytes,
+                                 hipStream_t stream);
+
 /* ------------------------------------------------------------------------
  * Kernel timing, a tracing aid.  While enabled on the calling thread, every
  * kernel launch made by the entry points above is bracketed by two HIP

@@ -38,7 +38,9 @@ EXPORTS = [
     "conduit_score_layers_workspace_bytes", "conduit_score_layers", "conduit_merge_refresh_attn",
     "conduit_rotary", "conduit_append_kv", "conduit_append_mx", "conduit_load_mx",
     "conduit_attn_mx_workspace_bytes", "conduit_attn_mx",
+    "conduit_append_byte", "conduit_load_byte", "conduit_attn_byte_workspace_bytes", "conduit_attn_byte",
 ]
+BYTE_BLOCK = 16  # tokens of the 8-bit cache that share a scale
 SCORE_NOALLOC_MAX_BYTES = 16 << 20
 
 
@@ -80,6 +82,10 @@ class KVMX(ctypes.Structure):
                 ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
                 ("table_stride", ctypes.c_int32), ("n_ctx", ctypes.c_int32), ("block_table", ctypes.c_void_p),
                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class KVByte(ctypes.Structure):
+    _fields_ = KVMX._fields_
 
 
 _lib = None
@@ -150,6 +156,15 @@ def lib() -> ctypes.CDLL:
         L.conduit_attn_mx_workspace_bytes.restype = sz
         L.conduit_attn_mx.argtypes = [pmx, vp, i32, vp, i32, f32, vp, vp, vp, sz, vp]
         L.conduit_attn_mx.restype = ctypes.c_int
+        pbyte = ctypes.POINTER(KVByte)
+        L.conduit_append_byte.argtypes = [pbyte, prows, vp, vp, prope, vp, i64, vp, vp, vp]
+        L.conduit_append_byte.restype = ctypes.c_int
+        L.conduit_load_byte.argtypes = [pbyte, vp, i32, pkv, vp, prope, vp, i64, vp]
+        L.conduit_load_byte.restype = ctypes.c_int
+        L.conduit_attn_byte_workspace_bytes.argtypes = [pbyte, i32, i32]
+        L.conduit_attn_byte_workspace_bytes.restype = sz
+        L.conduit_attn_byte.argtypes = [pbyte, vp, i32, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.conduit_attn_byte.restype = ctypes.c_int
         L.conduit_status_str.argtypes = [ctypes.c_int]
         L.conduit_status_str.restype = ctypes.c_char_p
         L.conduit_last_error.argtypes = []
@@ -519,6 +534,38 @@ def mx_desc(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: to
     return desc
 
 
+def byte_desc(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, n_q_heads: int,
+              n_ctx: Optional[int] = None, block_table: Optional[torch.Tensor] = None, n_seqs: int = 1) -> KVByte:
+    """Descriptor of one layer's 8-bit cache: k, v uint8 (or float8_e4m3fn) [n_pages,
+    H_kv, page, d] codes, k_scale, v_scale uint8 [n_pages, H_kv, page / 16] (pages evenly
+    strided, dense inside); block_table, n_ctx and n_seqs as in mx_desc."""
+    for t, dim in ((k, 4), (v, 4), (k_scale, 3), (v_scale, 3)):
+        codes = dim == 4 and t.dtype == torch.float8_e4m3fn
+        if (t.dtype != torch.uint8 and not codes) or t.dim() != dim or not t[:1].is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "pools must be uint8 [n_pages, H_kv, page, d] and "
+                                                "[n_pages, H_kv, page / 16], pages dense")
+    n_pages, hkv, page, d = k.shape
+    if v.shape != k.shape or v_scale.shape != k_scale.shape or k_scale.shape != (n_pages, hkv, page // BYTE_BLOCK) or \
+            page % BYTE_BLOCK:
+        raise ConduitError(ERR_INVALID_ARG, "the pools' shapes do not belong together")
+    if n_pages > 1 and (k.stride(0) != v.stride(0) or k_scale.stride(0) != v_scale.stride(0)):
+        raise ConduitError(ERR_INVALID_ARG, "k and v (and their scales) must have one page stride")
+    if block_table is not None:
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "block_table must be int32 [n_seqs, pages], dense")
+        n_seqs, table_stride = block_table.shape
+    else:
+        table_stride = n_pages // max(n_seqs, 1)
+    _one_device(k, v, k_scale, v_scale, block_table)
+    code_stride = k.stride(0) if n_pages > 1 else hkv * page * d
+    scale_stride = k_scale.stride(0) if n_pages > 1 else hkv * (page // BYTE_BLOCK)
+    desc = KVByte(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), code_stride, scale_stride,
+                  n_pages, page, n_seqs, table_stride, table_stride * page if n_ctx is None else n_ctx,
+                  _ptr(block_table), n_q_heads, hkv, d)
+    desc.tensors = (k, v, k_scale, v_scale, block_table)  # kept alive with the descriptor
+    return desc
+
+
 def _one_device(*tensors) -> int:
     """Index of the GPU that holds the tensors, -1 for the CPU."""
     dev = None
@@ -533,7 +580,7 @@ def _one_device(*tensors) -> int:
 
 
 def _held(desc) -> tuple:
-    """The tensors of a descriptor's cache, where mx_desc, kv_desc or kv_desc_paged made it."""
+    """The tensors of a descriptor's cache, where mx_desc, byte_desc, kv_desc or kv_desc_paged made it."""
     return getattr(desc, "tensors", ())
 
 
@@ -629,6 +676,12 @@ def conduit_append_kv(kv: KV, pos: torch.Tensor, k_new: torch.Tensor, v_new: tor
           ctypes.byref(kv), ctypes.byref(rows), _ptr(pos), desc, rp, ps)
 
 
+def _check_held_rows(k_new, k_out, v_out) -> None:
+    for t in (k_out, v_out):
+        if t is not None and (t.shape != k_new.shape or t.dtype != k_new.dtype or not t.is_contiguous()):
+            raise ConduitError(ERR_INVALID_ARG, "k_out and v_out must be dense and shaped like k_new")
+
+
 def conduit_append_mx(mx: KVMX, pos: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
                       rope: Optional[Rope] = None, rope_pos: Optional[torch.Tensor] = None,
                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -638,9 +691,7 @@ def conduit_append_mx(mx: KVMX, pos: torch.Tensor, k_new: torch.Tensor, v_new: t
     v_out [n, H_kv, d] receive the rows as the cache holds them; see
     conduit_append_mx."""
     rows = _new_rows(k_new, v_new, q, q_out, mx.n_q_heads, mx.n_kv_heads, mx.head_dim)
-    for t in (k_out, v_out):
-        if t is not None and (t.shape != k_new.shape or t.dtype != k_new.dtype or not t.is_contiguous()):
-            raise ConduitError(ERR_INVALID_ARG, "k_out and v_out must be dense and shaped like k_new")
+    _check_held_rows(k_new, k_out, v_out)
     desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
     _call(lib().conduit_append_mx,
           (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), rope_pos, *_held(mx)), stream,
@@ -658,6 +709,26 @@ def conduit_load_mx(mx: KVMX, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tens
           ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
 
 
+def _attn_pool(fn, need_fn, cache, q, pos, o_out, lse_out, scale, ws, stream) -> None:
+    """conduit_attn_mx or conduit_attn_byte with what both check."""
+    n = q.shape[0]
+    if q.shape != (n, cache.n_q_heads, cache.head_dim) or o_out.shape != q.shape or o_out.dtype != q.dtype or \
+            not q.is_contiguous() or not o_out.is_contiguous():
+        raise ConduitError(ERR_INVALID_ARG,
+                           f"q and o_out must be dense [n, {cache.n_q_heads}, {cache.head_dim}] of one dtype")
+    if lse_out is not None and (lse_out.shape != q.shape[:2] or lse_out.dtype != torch.float32 or
+                                not lse_out.is_contiguous()):
+        raise ConduitError(ERR_INVALID_ARG, "lse_out must be dense float32 [n, H_q]")
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.head_dim)
+    if ws is None:
+        need = need_fn(cache, q)
+        if need:
+            ws = _scratch(need, q.device, stream)
+    _call(fn, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws, *_held(cache)), stream, ctypes.byref(cache), _ptr(q),
+          _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
+
+
 def attn_mx_workspace_bytes(mx: KVMX, q: torch.Tensor) -> int:
     return int(lib().conduit_attn_mx_workspace_bytes(ctypes.byref(mx), q.shape[0], _dtype_code(q)))
 
@@ -667,21 +738,50 @@ def conduit_attn_mx(mx: KVMX, q: torch.Tensor, pos: torch.Tensor, o_out: torch.T
                     ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """Causal attention of rows over a 4-bit cache: q, o_out dense [n, H_q, d], pos
     int32 [n] (below 0: an empty row), lse_out fp32 [n, H_q]; see conduit_attn_mx."""
-    n = q.shape[0]
-    if q.shape != (n, mx.n_q_heads, mx.head_dim) or o_out.shape != q.shape or o_out.dtype != q.dtype or \
-            not q.is_contiguous() or not o_out.is_contiguous():
-        raise ConduitError(ERR_INVALID_ARG, f"q and o_out must be dense [n, {mx.n_q_heads}, {mx.head_dim}] of one dtype")
-    if lse_out is not None and (lse_out.shape != q.shape[:2] or lse_out.dtype != torch.float32 or
-                                not lse_out.is_contiguous()):
-        raise ConduitError(ERR_INVALID_ARG, "lse_out must be dense float32 [n, H_q]")
-    if scale is None:
-        scale = 1.0 / math.sqrt(mx.head_dim)
-    if ws is None:
-        need = attn_mx_workspace_bytes(mx, q)
-        if need:
-            ws = _scratch(need, q.device, stream)
-    _call(lib().conduit_attn_mx, (q, _row_ids(pos, n, "pos"), o_out, lse_out, ws, *_held(mx)), stream,
-          ctypes.byref(mx), _ptr(q), _dtype_code(q), _ptr(pos), n, scale, _ptr(o_out), _ptr(lse_out), _ptr(ws), _nbytes(ws))
+    _attn_pool(lib().conduit_attn_mx, attn_mx_workspace_bytes, mx, q, pos, o_out, lse_out, scale, ws, stream)
+
+
+def conduit_append_byte(cache: KVByte, pos: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                        n_held: Optional[torch.Tensor] = None, rope: Optional[Rope] = None,
+                        rope_pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                        v_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Tokens into an 8-bit cache (row i to sequence i // (n / n_seqs), positions
+    ascending): behind what it holds, or, with n_held int32 [n_seqs] (the tokens that each
+    sequence holds before the call), anywhere; k_out, v_out [n, H_kv, d] receive the rows as
+    the cache holds them; see conduit_append_byte."""
+    rows = _new_rows(k_new, v_new, q, q_out, cache.n_q_heads, cache.n_kv_heads, cache.head_dim)
+    _check_held_rows(k_new, k_out, v_out)
+    if n_held is not None:
+        _row_ids(n_held, cache.n_seqs, "n_held")
+    desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
+    _call(lib().conduit_append_byte,
+          (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), n_held, rope_pos, *_held(cache)), stream,
+          ctypes.byref(cache), ctypes.byref(rows), _ptr(pos), _ptr(n_held), desc, rp, ps, _ptr(k_out), _ptr(v_out))
+
+
+def conduit_load_byte(cache: KVByte, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tensor, rope: Optional[Rope] = None,
+                      rope_pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows of an 8-bit cache into a 16- or 32-bit cache, keys turned by how far they
+    move (rope_pos [n_axes, n]); see conduit_load_byte."""
+    n = src_pos.numel()
+    desc, rp, ps = _rope_args(rope, rope_pos, n)
+    ids = _row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos")
+    _call(lib().conduit_load_byte, (*ids, rope_pos, *_held(cache), *_held(kv)), stream, ctypes.byref(cache),
+          _ptr(src_pos), n, ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
+
+
+def attn_byte_workspace_bytes(cache: KVByte, q: torch.Tensor) -> int:
+    return int(lib().conduit_attn_byte_workspace_bytes(ctypes.byref(cache), q.shape[0], _dtype_code(q)))
+
+
+def conduit_attn_byte(cache: KVByte, q: torch.Tensor, pos: torch.Tensor, o_out: torch.Tensor,
+                      lse_out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                      ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of rows over an 8-bit cache, each to its sequence's tokens 0 .. pos[i]
+    (below 0: an empty row): q, o_out dense [n, H_q, d], pos int32 [n], lse_out fp32
+    [n, H_q]; see conduit_attn_byte."""
+    _attn_pool(lib().conduit_attn_byte, attn_byte_workspace_bytes, cache, q, pos, o_out, lse_out, scale, ws, stream)
 
 
 def profile_enable(enabled: bool) -> None:

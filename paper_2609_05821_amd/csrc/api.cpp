@@ -1196,6 +1196,8 @@ conduit_status conduit_refresh_attn_layers(const conduit_kv *kvs, int32_t n_laye
   return ok();
 }
 
+}  // extern "C"
+
 namespace {
 
 // The rope's table for kernel arguments; half = 0 (nothing turns) without one.
@@ -1306,12 +1308,18 @@ void cache_params(const conduit_kv *kv, RowParams *rp) {
   rp->n_ctx = kv->n_ctx;
 }
 
-conduit_status check_mx(const conduit_kv_mx *mx) {
-  if (!mx) return fail(CONDUIT_ERR_INVALID_ARG, "mx is NULL");
+// A cache of packed pools: conduit_kv_mx and conduit_kv_byte have the same fields.  token:
+// bytes of a token's codes per head; scales: scale bytes of a page per head.
+template <typename Desc>
+conduit_status check_pools(const Desc *mx, const char *name, int32_t (*token)(int32_t), int64_t (*scales)(const Desc *),
+                           int32_t scale_multiple) {
+  if (!mx) return fail(CONDUIT_ERR_INVALID_ARG, "%s is NULL", name);
   if (!mx->k || !mx->v || !mx->k_scale || !mx->v_scale)
-    return fail(CONDUIT_ERR_INVALID_ARG, "a pool of mx is NULL");
-  if (!aligned16(mx->k) || !aligned16(mx->v) || !aligned16(mx->k_scale) || !aligned16(mx->v_scale))
-    return fail(CONDUIT_ERR_INVALID_ARG, "the pools of mx must be 16-byte aligned");
+    return fail(CONDUIT_ERR_INVALID_ARG, "a pool of %s is NULL", name);
+  if (!aligned16(mx->k) || !aligned16(mx->v) ||
+      (reinterpret_cast<uintptr_t>(mx->k_scale) | reinterpret_cast<uintptr_t>(mx->v_scale)) % scale_multiple)
+    return fail(CONDUIT_ERR_INVALID_ARG, "the pools of %s must be 16-byte aligned (scales: %d-byte)", name,
+                scale_multiple);
   if (mx->n_kv_heads < 1 || mx->n_q_heads < 1) return fail(CONDUIT_ERR_INVALID_ARG, "head counts must be >= 1");
   if (mx->n_kv_heads > 256)
     return fail(CONDUIT_ERR_UNSUPPORTED, "n_kv_heads %d (supported: up to 256)", mx->n_kv_heads);
@@ -1327,13 +1335,14 @@ conduit_status check_mx(const conduit_kv_mx *mx) {
     return fail(CONDUIT_ERR_UNSUPPORTED, "page_size %d (supported: powers of two from 64 to 2^20)", ps);
   if (mx->n_pages < 1 || mx->n_seqs < 1 || mx->table_stride < 1)
     return fail(CONDUIT_ERR_INVALID_ARG, "n_pages, n_seqs and table_stride must be >= 1");
-  const int64_t page = (int64_t)mx->n_kv_heads * ps;
-  if (mx->code_stride < page * (mx->head_dim / 2) || mx->scale_stride < page * (mx->head_dim / 32))
+  const int64_t page_codes = (int64_t)mx->n_kv_heads * ps * token(mx->head_dim);
+  const int64_t page_scales = mx->n_kv_heads * scales(mx);
+  if (mx->code_stride < page_codes || mx->scale_stride < page_scales)
     return fail(CONDUIT_ERR_INVALID_ARG, "page strides (%lld, %lld) below a page of %lld codes and %lld scales",
-                (long long)mx->code_stride, (long long)mx->scale_stride, (long long)(page * (mx->head_dim / 2)),
-                (long long)(page * (mx->head_dim / 32)));
-  if (mx->code_stride % 16 || mx->scale_stride % 16)
-    return fail(CONDUIT_ERR_INVALID_ARG, "page strides must be multiples of 16 bytes");
+                (long long)mx->code_stride, (long long)mx->scale_stride, (long long)page_codes,
+                (long long)page_scales);
+  if (mx->code_stride % 16 || mx->scale_stride % scale_multiple)
+    return fail(CONDUIT_ERR_INVALID_ARG, "page strides must be multiples of 16 bytes (scales: of %d)", scale_multiple);
   if (mx->code_stride > INT64_MAX / mx->n_pages || mx->scale_stride > INT64_MAX / mx->n_pages)
     return fail(CONDUIT_ERR_INVALID_ARG, "n_pages times a page stride exceeds 64 bits");
   if (mx->n_ctx < 1 || mx->n_ctx > (int64_t)mx->table_stride * ps)
@@ -1348,8 +1357,20 @@ conduit_status check_mx(const conduit_kv_mx *mx) {
   return CONDUIT_OK;
 }
 
+conduit_status check_mx(const conduit_kv_mx *mx) {
+  return check_pools<conduit_kv_mx>(
+      mx, "mx", [](int32_t d) { return d / 2; },
+      [](const conduit_kv_mx *m) { return (int64_t)m->page_size * (m->head_dim / kMxBlock); }, 16);
+}
+conduit_status check_byte(const conduit_kv_byte *cache) {
+  return check_pools<conduit_kv_byte>(
+      cache, "cache", [](int32_t d) { return d; },
+      [](const conduit_kv_byte *m) { return (int64_t)m->page_size / kByteBlock; }, 4);
+}
+
 // n rows shared out over the sequences of a checked descriptor.
-conduit_status mx_cache(const conduit_kv_mx *mx, int32_t n, MxCache *c) {
+template <typename Desc>
+conduit_status mx_cache(const Desc *mx, int32_t n, MxCache *c) {
   if (n < 0 || n % mx->n_seqs)
     return fail(CONDUIT_ERR_INVALID_ARG, "n = %d rows are not a multiple of the %d sequences", n, mx->n_seqs);
   c->k = static_cast<uint8_t *>(mx->k);
@@ -1370,7 +1391,97 @@ conduit_status mx_cache(const conduit_kv_mx *mx, int32_t n, MxCache *c) {
 
 constexpr int64_t kMxMaxPairs = (int64_t(1) << 24) - 1;  // (a workgroup each: fewer than 2^32 threads)
 
+// Rows of a checked packed cache into kv.
+template <typename Desc>
+conduit_status load_rows(const Desc *mx, RowMode mode, const char *what, const int32_t *src_pos, int32_t n,
+                         const conduit_kv *kv, const int32_t *dst_pos, const conduit_rope *rope,
+                         const int32_t *rope_pos, int64_t rope_pos_stride, hipStream_t stream) {
+  conduit_status st = check_kv(kv);
+  RowParams rp{};
+  if (!st) st = mx_cache(mx, n, &rp.mx);
+  if (st) return st;
+  if (kv->n_kv_heads != mx->n_kv_heads || kv->head_dim != mx->head_dim)
+    return fail(CONDUIT_ERR_INVALID_ARG, "the caches differ in n_kv_heads or head_dim");
+  if (n == 0) return ok();
+  if (!src_pos || !dst_pos || reinterpret_cast<uintptr_t>(src_pos) % 4 || reinterpret_cast<uintptr_t>(dst_pos) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "src_pos and dst_pos must be non-NULL and 4-byte aligned");
+  st = check_heads(n, mx->n_kv_heads, mx->head_dim);
+  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, mx->head_dim, 0, 16, &rp.rope);
+  if (st) return st;
+  rp.n = n;
+  rp.n_kv_heads = mx->n_kv_heads;
+  rp.head_dim = mx->head_dim;
+  rp.pos = dst_pos;
+  rp.src_pos = src_pos;
+  cache_params(kv, &rp);
+  const hipError_t e = launch_rows(rp, mode, kv->dtype == CONDUIT_BF16, stream);
+  if (e != hipSuccess) return hip_fail(e, what);
+  return ok();
+}
+
+// Attention over a packed cache: how a call is cut up and how it is launched.
+typedef MxAttnShape (*AttnShapeFn)(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, bool);
+typedef hipError_t (*AttnLaunchFn)(const MxAttnParams &, const MxAttnShape &, int, bool, hipStream_t);
+
+template <typename Desc>
+size_t attn_workspace(const Desc *mx, AttnShapeFn shape, int32_t n, int32_t dtype) {
+  if (!mx || n < 1 || mx->n_seqs < 1 || n % mx->n_seqs || mx->n_kv_heads < 1 || mx->n_q_heads < mx->n_kv_heads ||
+      mx->n_ctx < 1 || (mx->head_dim != 64 && mx->head_dim != 128) || (int64_t)n * mx->n_q_heads > kMxMaxPairs)
+    return 0;
+  return shape(mx->n_seqs, n / mx->n_seqs, mx->n_q_heads, mx->n_kv_heads, mx->n_ctx, mx->head_dim,
+               dtype == CONDUIT_BF16).total;
+}
+
+// (mx is checked)
+template <typename Desc>
+conduit_status attn_rows(const Desc *mx, AttnShapeFn shape, AttnLaunchFn launch, const char *what, const void *q,
+                         int32_t dtype, const int32_t *pos, int32_t n, float scale, void *o_out, float *lse_out,
+                         void *ws, size_t ws_bytes, hipStream_t stream) {
+  MxAttnParams ap{};
+  conduit_status st = check_dtype(dtype);
+  if (!st) st = mx_cache(mx, n, &ap.mx);
+  if (st) return st;
+  if (!(scale >= 0x1p-126f && scale < 0x1p127f))
+    return fail(CONDUIT_ERR_INVALID_ARG, "scale %g outside [2^-126, 2^127)", scale);
+  if ((int64_t)n * mx->n_q_heads > kMxMaxPairs)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "n * n_q_heads = %lld exceeds %lld", (long long)n * mx->n_q_heads,
+                (long long)kMxMaxPairs);
+  if (n == 0) return ok();
+  if (!pos || reinterpret_cast<uintptr_t>(pos) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "pos must be non-NULL and 4-byte aligned");
+  if (!q || !aligned16(q) || !o_out || !aligned16(o_out))
+    return fail(CONDUIT_ERR_INVALID_ARG, "q and o_out must be non-NULL and 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(lse_out) % 4) return fail(CONDUIT_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
+  const bool bf16 = dtype == CONDUIT_BF16;
+  const MxAttnShape sh = shape(mx->n_seqs, ap.mx.rows_per_seq, mx->n_q_heads, mx->n_kv_heads, mx->n_ctx,
+                               mx->head_dim, bf16);
+  st = check_ws(ws, ws_bytes, sh.total);
+  if (st) return st;
+  ap.n_seqs = mx->n_seqs;
+  ap.n_q_heads = mx->n_q_heads;
+  ap.group = mx->n_q_heads / mx->n_kv_heads;
+  ap.blocks_per_seq = sh.blocks_per_seq;
+  ap.n_workers = sh.n_workers;
+  ap.q = q;
+  ap.pos = pos;
+  ap.scale_log2 = scale * kLog2e;
+  ap.o_out = o_out;
+  ap.lse_out = lse_out;
+  if (sh.total) {
+    ap.prefix = reinterpret_cast<int32_t *>(at(ws, sh.prefix));
+    ap.cut = reinterpret_cast<int32_t *>(at(ws, sh.parts));
+    ap.parts = ap.cut + 1;
+    ap.part_ml = reinterpret_cast<float2 *>(at(ws, sh.ml));
+    ap.part_o = reinterpret_cast<float *>(at(ws, sh.o));
+  }
+  const hipError_t e = launch(ap, sh, mx->head_dim, bf16, stream);
+  if (e != hipSuccess) return hip_fail(e, what);
+  return ok();
+}
+
 }  // namespace
+
+extern "C" {
 
 conduit_status conduit_rotary(const void *x, int64_t x_stride, int32_t n, int32_t n_heads, int32_t head_dim,
                               int32_t dtype, const conduit_rope *rope, const int32_t *rope_pos,
@@ -1449,85 +1560,74 @@ conduit_status conduit_append_mx(const conduit_kv_mx *mx, const conduit_rows *ro
   return ok();
 }
 
-conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, int32_t n, const conduit_kv *kv,
-                               const int32_t *dst_pos, const conduit_rope *rope, const int32_t *rope_pos,
-                               int64_t rope_pos_stride, hipStream_t stream) {
-  conduit_status st = check_mx(mx);
-  if (!st) st = check_kv(kv);
-  RowParams rp{};
-  if (!st) st = mx_cache(mx, n, &rp.mx);
+conduit_status conduit_append_byte(const conduit_kv_byte *cache, const conduit_rows *rows, const int32_t *pos,
+                                   const int32_t *n_held, const conduit_rope *rope, const int32_t *rope_pos,
+                                   int64_t rope_pos_stride, void *k_out, void *v_out, hipStream_t stream) {
+  conduit_status st = check_byte(cache);
   if (st) return st;
-  if (kv->n_kv_heads != mx->n_kv_heads || kv->head_dim != mx->head_dim)
-    return fail(CONDUIT_ERR_INVALID_ARG, "the caches differ in n_kv_heads or head_dim");
-  if (n == 0) return ok();
-  if (!src_pos || !dst_pos || reinterpret_cast<uintptr_t>(src_pos) % 4 || reinterpret_cast<uintptr_t>(dst_pos) % 4)
-    return fail(CONDUIT_ERR_INVALID_ARG, "src_pos and dst_pos must be non-NULL and 4-byte aligned");
-  st = check_heads(n, mx->n_kv_heads, mx->head_dim);
-  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, n, mx->head_dim, 0, 16, &rp.rope);
+  if (!rows) return fail(CONDUIT_ERR_INVALID_ARG, "rows is NULL");
+  st = check_dtype(rows->dtype);
+  ByteAppendParams ap{};
+  if (!st) st = mx_cache(cache, rows->n, &ap.rows.mx);
   if (st) return st;
-  rp.n = n;
-  rp.n_kv_heads = mx->n_kv_heads;
-  rp.head_dim = mx->head_dim;
-  rp.pos = dst_pos;
-  rp.src_pos = src_pos;
-  cache_params(kv, &rp);
-  const hipError_t e = launch_rows(rp, kRowLoadMx, kv->dtype == CONDUIT_BF16, stream);
-  if (e != hipSuccess) return hip_fail(e, "load from 4 bits");
+  if (rows->n == 0) return ok();
+  st = check_new_rows(rows, pos, cache->n_q_heads, cache->n_kv_heads, cache->head_dim, &ap.rows);
+  if (!st) st = rope_table(rope, rope_pos, rope_pos_stride, rows->n, cache->head_dim, 0, 16, &ap.rows.rope);
+  if (!st && reinterpret_cast<uintptr_t>(n_held) % 4)
+    st = fail(CONDUIT_ERR_INVALID_ARG, "n_held must be 4-byte aligned");
+  if (!st && ((k_out && !aligned16(k_out)) || (v_out && !aligned16(v_out))))
+    st = fail(CONDUIT_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  if (st) return st;
+  ap.n_held = n_held;
+  ap.rows.k_out = k_out;
+  ap.rows.v_out = v_out;
+  const hipError_t e = launch_append_byte(ap, rows->dtype == CONDUIT_BF16, stream);
+  if (e != hipSuccess) return hip_fail(e, "append in 8 bits");
   return ok();
 }
 
+conduit_status conduit_load_mx(const conduit_kv_mx *mx, const int32_t *src_pos, int32_t n, const conduit_kv *kv,
+                               const int32_t *dst_pos, const conduit_rope *rope, const int32_t *rope_pos,
+                               int64_t rope_pos_stride, hipStream_t stream) {
+  const conduit_status st = check_mx(mx);
+  if (st) return st;
+  return load_rows(mx, kRowLoadMx, "load from 4 bits", src_pos, n, kv, dst_pos, rope, rope_pos, rope_pos_stride,
+                   stream);
+}
+
+conduit_status conduit_load_byte(const conduit_kv_byte *cache, const int32_t *src_pos, int32_t n, const conduit_kv *kv,
+                                 const int32_t *dst_pos, const conduit_rope *rope, const int32_t *rope_pos,
+                                 int64_t rope_pos_stride, hipStream_t stream) {
+  const conduit_status st = check_byte(cache);
+  if (st) return st;
+  return load_rows(cache, kRowLoadByte, "load from 8 bits", src_pos, n, kv, dst_pos, rope, rope_pos, rope_pos_stride,
+                   stream);
+}
+
 size_t conduit_attn_mx_workspace_bytes(const conduit_kv_mx *mx, int32_t n, int32_t dtype) {
-  if (!mx || n < 1 || mx->n_seqs < 1 || n % mx->n_seqs || mx->n_kv_heads < 1 || mx->n_q_heads < mx->n_kv_heads ||
-      mx->n_ctx < 1 || (mx->head_dim != 64 && mx->head_dim != 128) || (int64_t)n * mx->n_q_heads > kMxMaxPairs)
-    return 0;
-  return mx_attn_shape(mx->n_seqs, n / mx->n_seqs, mx->n_q_heads, mx->n_kv_heads, mx->n_ctx, mx->head_dim,
-                       dtype == CONDUIT_BF16).total;
+  return attn_workspace(mx, mx_attn_shape, n, dtype);
 }
 
 conduit_status conduit_attn_mx(const conduit_kv_mx *mx, const void *q, int32_t dtype, const int32_t *pos, int32_t n,
                                float scale, void *o_out, float *lse_out, void *ws, size_t ws_bytes,
                                hipStream_t stream) {
-  conduit_status st = check_mx(mx);
-  MxAttnParams ap{};
-  if (!st) st = check_dtype(dtype);
-  if (!st) st = mx_cache(mx, n, &ap.mx);
+  const conduit_status st = check_mx(mx);
   if (st) return st;
-  if (!(scale >= 0x1p-126f && scale < 0x1p127f))
-    return fail(CONDUIT_ERR_INVALID_ARG, "scale %g outside [2^-126, 2^127)", scale);
-  if ((int64_t)n * mx->n_q_heads > kMxMaxPairs)
-    return fail(CONDUIT_ERR_UNSUPPORTED, "n * n_q_heads = %lld exceeds %lld", (long long)n * mx->n_q_heads,
-                (long long)kMxMaxPairs);
-  if (n == 0) return ok();
-  if (!pos || reinterpret_cast<uintptr_t>(pos) % 4)
-    return fail(CONDUIT_ERR_INVALID_ARG, "pos must be non-NULL and 4-byte aligned");
-  if (!q || !aligned16(q) || !o_out || !aligned16(o_out))
-    return fail(CONDUIT_ERR_INVALID_ARG, "q and o_out must be non-NULL and 16-byte aligned");
-  if (reinterpret_cast<uintptr_t>(lse_out) % 4) return fail(CONDUIT_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
-  const bool bf16 = dtype == CONDUIT_BF16;
-  const MxAttnShape sh = mx_attn_shape(mx->n_seqs, ap.mx.rows_per_seq, mx->n_q_heads, mx->n_kv_heads, mx->n_ctx,
-                                       mx->head_dim, bf16);
-  st = check_ws(ws, ws_bytes, sh.total);
+  return attn_rows(mx, mx_attn_shape, launch_attn_mx, "attention over 4 bits", q, dtype, pos, n, scale, o_out, lse_out,
+                   ws, ws_bytes, stream);
+}
+
+size_t conduit_attn_byte_workspace_bytes(const conduit_kv_byte *cache, int32_t n, int32_t dtype) {
+  return attn_workspace(cache, byte_attn_shape, n, dtype);
+}
+
+conduit_status conduit_attn_byte(const conduit_kv_byte *cache, const void *q, int32_t dtype, const int32_t *pos,
+                                 int32_t n, float scale, void *o_out, float *lse_out, void *ws, size_t ws_bytes,
+                                 hipStream_t stream) {
+  const conduit_status st = check_byte(cache);
   if (st) return st;
-  ap.n_seqs = mx->n_seqs;
-  ap.n_q_heads = mx->n_q_heads;
-  ap.group = mx->n_q_heads / mx->n_kv_heads;
-  ap.blocks_per_seq = sh.blocks_per_seq;
-  ap.n_workers = sh.n_workers;
-  ap.q = q;
-  ap.pos = pos;
-  ap.scale_log2 = scale * kLog2e;
-  ap.o_out = o_out;
-  ap.lse_out = lse_out;
-  if (sh.total) {
-    ap.prefix = reinterpret_cast<int32_t *>(at(ws, sh.prefix));
-    ap.cut = reinterpret_cast<int32_t *>(at(ws, sh.parts));
-    ap.parts = ap.cut + 1;
-    ap.part_ml = reinterpret_cast<float2 *>(at(ws, sh.ml));
-    ap.part_o = reinterpret_cast<float *>(at(ws, sh.o));
-  }
-  const hipError_t e = launch_attn_mx(ap, sh, mx->head_dim, bf16, stream);
-  if (e != hipSuccess) return hip_fail(e, "attention over 4 bits");
-  return ok();
+  return attn_rows(cache, byte_attn_shape, launch_attn_byte, "attention over 8 bits", q, dtype, pos, n, scale, o_out,
+                   lse_out, ws, ws_bytes, stream);
 }
 
 const char *conduit_status_str(conduit_status status) {

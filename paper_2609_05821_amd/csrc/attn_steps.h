@@ -1,0 +1,366 @@
+// What attention over the 4-bit and the 8-bit cache shares (attn_mx.hip,
+// attn_byte.hip): how the key steps of a call are listed and shared out over
+// workgroups, how pages are looked up, exact bf16 parts of fp32 numbers, and the
+// launch that joins blocks which were cut.
+#pragma once
+
+#include <algorithm>
+
+#include "mx.h"
+
+namespace conduit {
+namespace {
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kMInit = -1e30f;  // initial running maximum (log2 units)
+// The running maximum moves when a step exceeds it by more than this many log2
+// units; probabilities stay below 2^8.  Exact: sum and output share it.
+constexpr float kSlack = 8.f;
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kWaveKeys = 32;
+constexpr int kStep = kWaves * kWaveKeys;  // keys of a workgroup step
+
+// Many pairs per KV head: keys of a tile, pairs of a block, and LDS of a workgroup.
+constexpr int kTileKeys = 64;
+constexpr int kManyPairs = 32 * kWaves;
+
+template <int NS>
+struct Parts {
+  bf16x8 v[NS];
+};
+
+// x as the sum of NS bf16 parts, each the nearest to what those before it leave
+// (half a step is up to 2^-8 of a value): three are exact, two up to 2^-17 of x off.
+// WIDE: the first part is cut off instead (16 of 24 bits are left, which two parts hold),
+// because the largest x would round up to an infinity.
+template <int NS, bool WIDE = false>
+__device__ __forceinline__ void split_parts(const float (&x)[8], Parts<NS> &out) {
+  float r[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = x[j];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      __bf16 b = static_cast<__bf16>(r[j]);
+      if (WIDE && s == 0) {
+        const u16 top = (u16)(__builtin_bit_cast(uint32_t, r[j]) >> 16);
+        b = __builtin_bit_cast(__bf16, top);
+      }
+      out.v[s][j] = b;
+      if (s + 1 < NS) r[j] -= (float)b;
+    }
+}
+
+__device__ __forceinline__ float scale_of(int byte) { return __builtin_bit_cast(float, (uint32_t)byte << 23); }
+
+__device__ __forceinline__ int wave_max_i(int x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x = max(x, __shfl_xor(x, o, 64));
+  return x;
+}
+__device__ __forceinline__ int wave_min_i(int x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x = min(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+// Keys 0 .. n - 1 that a row at position `pos` may see, n <= n_ctx.
+__device__ __forceinline__ int keys_seen(int pos, int n_ctx) { return min(max(pos, -1), n_ctx - 1) + 1; }
+
+// Steps of `step` keys of sequence block sb for one KV head (positions loaded
+// eight at a time).
+__device__ __forceinline__ int block_steps(const MxAttnParams &p, int sb, int pairs, int step) {
+  const int s = sb / p.blocks_per_seq, rb = sb - s * p.blocks_per_seq, r = p.mx.rows_per_seq;
+  const int lo = rb * pairs / p.group, hi = min((rb * pairs + pairs - 1) / p.group, r - 1);
+  const int32_t *pos = p.pos + (int64_t)s * r;
+  int top = -1;
+  for (int i = lo; i <= hi; i += 8) {
+    int x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = pos[min(i + j, hi)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, x[j]);
+  }
+  return (keys_seen(top, p.mx.n_ctx) + step - 1) / step;
+}
+
+// Workgroups that share `total` steps: no fewer than kMinSteps each.
+constexpr int kMinSteps = 2;
+__device__ __forceinline__ int workers(int n_workers, int total) { return min(n_workers, max(1, total / kMinSteps)); }
+__device__ __forceinline__ int part_begin(int w, int total, int n) { return (int)((int64_t)w * total / n); }
+
+// The list of key steps of the whole call (sequence block by sequence block and
+// there KV head by KV head) and what of it is this workgroup's; workgroup 0 keeps
+// the list for the merge.  With up to 64 sequence blocks every wave makes the list
+// for itself, a block a lane; with more the workgroup makes it in LDS.
+//
+// Equal parts may begin in one block and end in the next, and what ends and
+// begins there costs a workgroup as much as three steps.  Where parts of up to
+// kOver steps more than equal ones can be cut block by block for the workgroups at
+// hand, they are (`cut`: their length).  8 sequences of up to 8,192 keys with 5 rows
+// 26.0 -> 23.3 us, one of 4,096 with 200 rows 39.5 -> 36.1.
+constexpr int kOver = 2;
+constexpr int kLaneBlocks = 64;
+struct Part {
+  int t, t_end;              // places in the list: steps, or with cut parts
+  int cut;
+  int before, after, steps;  // up to kLaneBlocks: the lane's block in the list, and its steps per head
+};
+__device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int step, int *s_sum, int *s_prefix,
+                                          Part &part) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_sb = p.n_seqs * p.blocks_per_seq, hkv = p.mx.n_kv_heads, w = blockIdx.x;
+  int total = 0;
+  if (n_sb <= kLaneBlocks) {
+    part.steps = lane < n_sb ? block_steps(p, lane, pairs, step) : 0;
+    int own = part.steps * hkv;
+    part.after = (int)wave_inclusive_sum((uint32_t)own);
+    part.before = part.after - own;
+    total = __builtin_amdgcn_readlane(part.after, 63);
+    if (w == 0 && wave == 0) {
+      if (lane < n_sb) p.prefix[lane] = part.before;
+      if (lane == 0) p.prefix[n_sb] = total;
+    }
+    const int n = workers(p.n_workers, total), equal = max(1, (total + n - 1) / n);
+    for (int x = equal; x <= equal + kOver; ++x) {
+      own = (part.steps + x - 1) / x * hkv;
+      const int incl = (int)wave_inclusive_sum((uint32_t)own), all = __builtin_amdgcn_readlane(incl, 63);
+      if (all <= p.n_workers) {
+        part.cut = x;
+        part.after = incl;
+        part.before = incl - own;
+        part.t = w;
+        part.t_end = min(w + 1, all);
+        break;
+      }
+    }
+    if (w == 0 && wave == 0) {
+      if (lane == 0) *p.cut = part.cut;
+      if (lane < n_sb) p.parts[lane] = part.before;
+    }
+    if (part.cut) return part.t < part.t_end;
+  } else {
+    for (int b0 = 0; b0 < n_sb; b0 += kThreads) {
+      const int sb = b0 + tid;
+      const int own = sb < n_sb ? block_steps(p, sb, pairs, step) * hkv : 0;
+      const int incl = (int)wave_inclusive_sum((uint32_t)own);
+      __syncthreads();
+      if (lane == 63) s_sum[wave] = incl;
+      __syncthreads();
+      int before = total;
+      for (int i = 0; i < kWaves; ++i) {
+        if (i < wave) before += s_sum[i];
+        total += s_sum[i];
+      }
+      if (sb < n_sb) s_prefix[sb] = before + incl - own;
+    }
+    if (tid == 0) s_prefix[n_sb] = total;
+    __syncthreads();
+    if (w == 0) {
+      for (int i = tid; i <= n_sb; i += kThreads) p.prefix[i] = s_prefix[i];
+      if (tid == 0) *p.cut = 0;
+    }
+  }
+  const int n = workers(p.n_workers, total);
+  if (w >= n) return false;
+  part.t = __builtin_amdgcn_readfirstlane(part_begin(w, total, n));
+  part.t_end = __builtin_amdgcn_readfirstlane(part_begin(w + 1, total, n));
+  return true;
+}
+
+// What of a part lies in one (sequence block, KV head): its steps [first, last)
+// of `steps`.
+struct Segment {
+  int sb, h, first, last, steps;
+};
+__device__ __forceinline__ Segment segment_at(const MxAttnParams &p, int n_sb, const int *s_prefix, const Part &part) {
+  int sb, begin, steps;
+  if (n_sb <= kLaneBlocks) {
+    sb = (int)__builtin_popcountll(__ballot(part.after <= part.t));
+    begin = __builtin_amdgcn_readlane(part.before, sb);
+    steps = __builtin_amdgcn_readlane(part.steps, sb);
+  } else {
+    int lo = 0, hi = n_sb - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (s_prefix[mid + 1] > part.t) hi = mid;
+      else lo = mid + 1;
+    }
+    sb = __builtin_amdgcn_readfirstlane(lo);
+    begin = __builtin_amdgcn_readfirstlane(s_prefix[lo]);
+    steps = __builtin_amdgcn_readfirstlane((s_prefix[lo + 1] - begin) / p.mx.n_kv_heads);
+  }
+  const int per_head = part.cut ? (steps + part.cut - 1) / part.cut : steps, at = part.t - begin;
+  const int h = at / per_head, rest = at - h * per_head;
+  const int first = part.cut ? rest * part.cut : rest;
+  return {sb, h, first, min(steps, first + (part.cut ? part.cut : part.t_end - part.t)), steps};
+}
+
+// Pages of one sequence, looked up in two parts: the block-table entry is loaded
+// well before it is made a page number.  (A load whose address is the same in
+// every lane would be made scalar, and waited for, at once: the lane's offset is
+// hidden from the compiler.  That wait, for every load in flight, was 1 us a tile.)
+struct SeqPages {
+  __amdgpu_buffer_rsrc_t table;
+  int first;     // page of token 0 without a table
+  bool listed;
+};
+__device__ __forceinline__ SeqPages seq_pages(const MxCache &c, int seq) {
+  const int64_t first = (int64_t)seq * c.table_stride;
+  SeqPages r;
+  r.listed = c.table != nullptr;
+  r.first = (int)first;
+  // (2^24 pages hold 2^30 tokens; a read past the end returns 0)
+  r.table = buffer_rsrc(r.listed ? c.table + first : nullptr, r.listed ? min(c.table_stride, 1 << 24) * 4 : 0);
+  return r;
+}
+__device__ __forceinline__ int page_entry(const SeqPages &s, int i) {
+  int off = i * 4;
+  asm("" : "+v"(off));
+  return __builtin_amdgcn_raw_buffer_load_b32(s.table, off, 0, 0);
+}
+__device__ __forceinline__ int page_number(const MxCache &c, const SeqPages &s, int i, int entry) {
+  const int page = s.listed ? __builtin_amdgcn_readfirstlane(entry) : s.first + i;
+  return min(max(page, 0), c.n_pages - 1);
+}
+
+// Merge of the blocks that more than one workgroup worked on, and the outputs
+// of blocks without keys.  A workgroup takes PW pairs of a block, a group of D / 4
+// lanes each; with PW = 1 all groups share the parts of one pair.
+template <int D, bool BF16, int PW>
+__global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int pairs) {
+  constexpr int L4 = D / 4;          // lanes of a part
+  constexpr int kGroups = 256 / L4, kShare = kGroups / PW;
+  // Parts a group has on their way at a time: where a workgroup shares one pair's,
+  // there may be a hundred (one sequence of 65,536 keys, both launches: one at a
+  // time 23.8 us, four 19.9).
+  constexpr int kBatch = PW == 1 ? 4 : 1;
+  __shared__ float s_m[kGroups], s_l[kGroups];
+  __shared__ f32x4 s_o[kShare > 1 ? kGroups : 1][L4];
+  const int chunks = (min(pairs, p.mx.rows_per_seq * p.group) + PW - 1) / PW, hkv = p.mx.n_kv_heads;
+  const int sb = blockIdx.x / (chunks * hkv), rest = blockIdx.x - sb * (chunks * hkv);
+  const int h = rest / chunks, chunk = rest - h * chunks;
+  const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
+  const int grp = threadIdx.x / L4, share = grp / PW, e = (threadIdx.x % L4) * 4;
+  const int j = chunk * PW + grp % PW, pair = rb * pairs + j;
+  const bool out = pair < p.mx.rows_per_seq * p.group;
+  if (rb * pairs + chunk * PW >= p.mx.rows_per_seq * p.group) return;
+  const int base = p.prefix[sb], next = p.prefix[sb + 1], total = p.prefix[p.n_seqs * p.blocks_per_seq];
+  const int cut = *p.cut;
+  const int n = workers(p.n_workers, total), steps = (next - base) / hkv;
+  float M = kMInit, L = 0.f;
+  f32x4 o{};
+  if (steps > 0) {
+    // The workgroup that holds step x is the last whose part begins at or
+    // before it (doubles: exact below 2^53, quotients far from rounding up).
+    const int t0 = base + h * steps, t1 = t0 + steps;
+    int w0 = (int)(((double)(t0 + 1) * n - 1) / total), w1 = (int)(((double)t1 * n - 1) / total);
+    int first = 2 * w0 + (part_begin(w0, total, n) >= t0 ? 0 : 1);
+    if (cut) {
+      const int parts = (steps + cut - 1) / cut;
+      w0 = p.parts[sb] + h * parts;
+      w1 = w0 + parts - 1;
+      first = 2 * w0;
+    }
+    if (w0 == w1) return;  // written by that workgroup
+    if (out)
+      for (int w = w0 + share; w <= w1; w += kBatch * kShare) {
+        float2 ml[kBatch];
+        f32x4 x[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int wi = w + i * kShare;
+          ml[i] = make_float2(kMInit, 0.f);
+          x[i] = f32x4{};
+          if (wi <= w1) {
+            const int64_t slot = wi == w0 ? first : 2 * wi;
+            ml[i] = p.part_ml[slot * pairs + j];
+            x[i] = *reinterpret_cast<const f32x4 *>(p.part_o + (slot * pairs + j) * D + e);
+          }
+        }
+        float mn = M;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) mn = fmaxf(mn, ml[i].x);
+        const float a = fast_exp2(M - mn);
+        M = mn;
+        L *= a;
+        o *= a;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float b = fast_exp2(ml[i].x - mn);
+          L += ml[i].y * b;
+          o += x[i] * b;
+        }
+      }
+  }
+  if constexpr (kShare > 1) {
+    s_o[grp][threadIdx.x % L4] = o;
+    if (e == 0) {
+      s_m[grp] = M;
+      s_l[grp] = L;
+    }
+    __syncthreads();
+    if (share) return;
+    for (int i = PW + grp; i < kGroups; i += PW) {
+      const float mn = fmaxf(M, s_m[i]), a = fast_exp2(M - mn), b = fast_exp2(s_m[i] - mn);
+      M = mn;
+      L = L * a + s_l[i] * b;
+      o = o * a + s_o[i][threadIdx.x % L4] * b;
+    }
+  }
+  if (!out) return;
+  o *= L == 0.f ? 0.f : 1.f / L;
+  const int64_t gp = ((int64_t)seq * p.mx.rows_per_seq + pair / p.group) * p.n_q_heads + h * p.group + pair % p.group;
+  if constexpr (BF16) {
+    *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
+        make_ushort4(f32_to_bf16(o[0]), f32_to_bf16(o[1]), f32_to_bf16(o[2]), f32_to_bf16(o[3]));
+  } else {
+    *reinterpret_cast<f32x4 *>(static_cast<float *>(p.o_out) + gp * D + e) = o;
+  }
+  if (e == 0 && p.lse_out) p.lse_out[gp] = L == 0.f ? kNegInf : (M + __log2f(L)) * kLn2;
+}
+
+template <int D, int PW>
+void launch_merge(const MxAttnParams &p, const MxAttnShape &sh, int blocks, bool few, bool bf16, hipStream_t s) {
+  const int pairs = std::min(sh.pairs, p.mx.rows_per_seq * p.group);  // of the largest block
+  const int grid = blocks * (few ? pairs : (pairs + PW - 1) / PW);
+  if (few)
+    bf16 ? attn_mx_merge_kernel<D, true, 1><<<grid, 256, 0, s>>>(p, sh.pairs)
+         : attn_mx_merge_kernel<D, false, 1><<<grid, 256, 0, s>>>(p, sh.pairs);
+  else
+    attn_mx_merge_kernel<D, true, PW><<<grid, 256, 0, s>>>(p, sh.pairs);
+}
+
+// Workspace of a call whose workgroups share the steps.
+inline void lay_out_workspace(MxAttnShape &L, int64_t n_sb, int head_dim) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
+  if (L.n_workers) {
+    const size_t slots = 2 * (size_t)L.n_workers * L.pairs;
+    L.prefix = take((size_t)(n_sb + 1) * 4);
+    L.parts = take((size_t)(kLaneBlocks + 1) * 4);
+    L.ml = take(slots * 8);
+    L.o = take(slots * head_dim * 4);
+  }
+  L.total = off;
+}
+
+// The launch that merges, where workgroups share the steps.  Few pairs: many parts of
+// each, shared out over a workgroup; many pairs: a few parts of each, one group of lanes.
+inline hipError_t launch_attn_merge(const MxAttnParams &p, const MxAttnShape &sh, const char *name, int head_dim,
+                                    bool bf16, hipStream_t s) {
+  ProfScope ps(name, s);
+  const int blocks = p.n_seqs * p.blocks_per_seq * p.mx.n_kv_heads;
+  const bool few = sh.pairs <= 32 || p.n_workers > 4 * blocks;
+  if (head_dim == 128)
+    launch_merge<128, 8>(p, sh, blocks, few, bf16, s);
+  else
+    launch_merge<64, 16>(p, sh, blocks, few, bf16, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace conduit

@@ -1,5 +1,6 @@
-// Internal declarations of rotary positions, growing caches and the 4-bit
-// cache (rotary.hip, attn_mx.hip and the host layer).
+// Internal declarations of rotary positions, growing caches and the 4-bit and
+// 8-bit caches (rotary.hip, append_byte.hip, attn_mx.hip, attn_byte.hip and the host
+// layer).
 #pragma once
 
 #include "common.h"
@@ -19,7 +20,8 @@ struct RopeTable {
   uint8_t axis[kMaxRotHalf];
 };
 
-// The 4-bit cache (conduit_kv_mx).
+// The 4-bit cache (conduit_kv_mx) or the 8-bit one (conduit_kv_byte): they differ in
+// the bytes of a token's codes and in what shares a scale.
 struct MxCache {
   uint8_t *k, *v;
   uint8_t *k_scale, *v_scale;
@@ -45,12 +47,31 @@ constexpr int kMxScaleMin = 2;    // smallest and largest scale byte written
 constexpr int kMxScaleMax = 252;
 constexpr int kMxScaleNan = 255;
 
+constexpr int kByteBlock = 16;      // tokens of the 8-bit cache that share a scale
+constexpr int kByteScaleMin = 10;   // smallest and largest scale byte written
+constexpr int kByteScaleMax = 246;
+
+// The factor of a scale byte of the 8-bit cache.  Bytes that no append writes are
+// read as the nearest that one does.
+__device__ __forceinline__ float byte_scale(int byte) {
+  return __builtin_bit_cast(float, (uint32_t)min(max(byte, kByteScaleMin), kByteScaleMax) << 23);
+}
+
+// Orders this wave's LDS writes before its reads (and the other way round) for
+// the compiler; the hardware keeps a wave's LDS accesses in order.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // What a launch of the row kernel does with its rows.
 enum RowMode {
   kRowTurn = 0,      // queries only (conduit_rotary)
   kRowAppend = 1,    // and keys and values into a cache of 16 or 32 bits
   kRowAppendMx = 2,  // and keys and values into a 4-bit cache
-  kRowLoadMx = 3     // rows of a 4-bit cache into a cache of 16 or 32 bits
+  kRowLoadMx = 3,    // rows of a 4-bit cache into a cache of 16 or 32 bits
+  kRowLoadByte = 4     // rows of an 8-bit cache into a cache of 16 or 32 bits
 };
 
 struct RowParams {
@@ -63,19 +84,26 @@ struct RowParams {
   int64_t q_stride, q_out_stride;       // elements
   const void *k_new, *v_new;            // kRowAppend, kRowAppendMx
   int64_t k_new_stride, v_new_stride;
-  const int32_t *pos;                   // place in the cache (kRowLoadMx: in kv)
-  const int32_t *src_pos;               // kRowLoadMx: place in mx
-  void *k, *v;                          // kRowAppend, kRowLoadMx: the cache
+  const int32_t *pos;                   // place in the cache (loads: in kv)
+  const int32_t *src_pos;               // kRowLoadMx, kRowLoadByte: place in mx
+  void *k, *v;                          // kRowAppend, loads: the cache
   int64_t k_stride, v_stride;
   KvPages pages;
   int32_t n_ctx;
-  MxCache mx;                           // kRowAppendMx, kRowLoadMx
+  MxCache mx;                           // kRowAppendMx, kRowLoadMx, kRowLoadByte
   void *k_out, *v_out;                  // kRowAppendMx, nullable: the rows as held
   RopeTable rope;
 };
 hipError_t launch_rows(const RowParams &p, RowMode mode, bool bf16, hipStream_t s);
 
-// Attention over a 4-bit cache.
+// New rows into an 8-bit cache (RowParams without kv; rope may turn).
+struct ByteAppendParams {
+  RowParams rows;               // n, heads, new rows, positions, mx, k_out, v_out, rope
+  const int32_t *n_held;        // nullable [n / rows.mx.rows_per_seq]: tokens held before
+};
+hipError_t launch_append_byte(const ByteAppendParams &p, bool bf16, hipStream_t s);
+
+// Attention over a 4-bit or an 8-bit cache.
 struct MxAttnParams {
   MxCache mx;
   int32_t n_seqs;
@@ -105,5 +133,8 @@ struct MxAttnShape {
 MxAttnShape mx_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_ctx,
                           int32_t head_dim, bool bf16);
 hipError_t launch_attn_mx(const MxAttnParams &p, const MxAttnShape &shape, int head_dim, bool bf16, hipStream_t s);
+MxAttnShape byte_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_ctx,
+                          int32_t head_dim, bool bf16);
+hipError_t launch_attn_byte(const MxAttnParams &p, const MxAttnShape &shape, int head_dim, bool bf16, hipStream_t s);
 
 }  // namespace conduit

@@ -1,5 +1,5 @@
 // Rotary positions, appends to caches of 16, 32 and 4 bits, and loads from the
-// 4-bit cache, gfx950.
+// 4-bit and the 8-bit cache, gfx950.
 //
 // One kernel body serves all of them.  The heads of all rows are one list; a wave
 // takes one or two times as many as its 64 lanes hold, issues all their loads,
@@ -23,14 +23,14 @@
 // fp32 error of an angle or a product can move a value over a border between
 // two codes.
 #include <algorithm>
+#include <type_traits>
 
-#include "mx.h"
+#include "rows.h"
 
 namespace conduit {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVec = 8;  // dims of a lane
 constexpr int kWaves = kThreads / 64;
 // Heads of a wave in units of what its lanes hold, where a row has as many: their
 // angles are shared.  17,024 rows of 36 heads: 1 unit 67 us, 2 units 62; with 64 of
@@ -38,128 +38,7 @@ constexpr int kWaves = kThreads / 64;
 // registers), so 1 there.  With few rows 1 keeps more waves busy.
 constexpr int kMany = 2;
 constexpr int64_t kManyFrom = 8192;  // units of work from which on
-constexpr int kDppQuad0011 = 0x50, kDppQuad2233 = 0xFA;  // lane i of four <- that of the four
 constexpr int kDppShl4 = 0x104;  // lane i <- lane i + 4 of its 16
-typedef double f64x2 __attribute__((ext_vector_type(2)));
-
-// (cos, sin) of a = p * f: a is reduced by the nearest multiple of pi/2 (two-part
-// constant, fused multiply-adds), then Taylor series on [-pi/4, pi/4], whose
-// first omitted terms are below 5e-17.
-__device__ __forceinline__ f64x2 cos_sin(double a) {
-  // (1.5 * 2^52 leaves the integer in the low bits; |a| < 2^41.01)
-  const double shifted = __builtin_fma(a, 0.63661977236758134308, 6755399441055744.0);
-  const double k = shifted - 6755399441055744.0;
-  double r = __builtin_fma(-k, 1.57079632679489655800e+00, a);
-  r = __builtin_fma(-k, 6.12323399573676603587e-17, r);
-  const double z = r * r;
-  double s = -1.0 / 1307674368000.0;                        // 1/15!
-  s = __builtin_fma(s, z, 1.0 / 6227020800.0);              // 1/13!
-  s = __builtin_fma(s, z, -1.0 / 39916800.0);
-  s = __builtin_fma(s, z, 1.0 / 362880.0);
-  s = __builtin_fma(s, z, -1.0 / 5040.0);
-  s = __builtin_fma(s, z, 1.0 / 120.0);
-  s = __builtin_fma(s, z, -1.0 / 6.0);
-  s = __builtin_fma(s * z, r, r);
-  double c = 1.0 / 20922789888000.0;                        // 1/16!
-  c = __builtin_fma(c, z, -1.0 / 87178291200.0);            // 1/14!
-  c = __builtin_fma(c, z, 1.0 / 479001600.0);
-  c = __builtin_fma(c, z, -1.0 / 3628800.0);
-  c = __builtin_fma(c, z, 1.0 / 40320.0);
-  c = __builtin_fma(c, z, -1.0 / 720.0);
-  c = __builtin_fma(c, z, 1.0 / 24.0);
-  c = __builtin_fma(c, z, -0.5);
-  c = __builtin_fma(c, z, 1.0);
-  const int q = (int)__builtin_bit_cast(uint64_t, shifted) & 3;  // k mod 4
-  const double cc = q & 1 ? s : c, ss = q & 1 ? c : s;
-  return f64x2{q == 1 || q == 2 ? -cc : cc, q >= 2 ? -ss : ss};
-}
-
-// 8 elements as loaded, and their values.
-template <typename T>
-struct Raw {
-  u32x4 w[sizeof(T) / 2];
-};
-// (fp32: the second four are `gap` elements after the first)
-template <typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T *p, int gap = 4) {
-  Raw<T> r;
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ld16(p + gap * i);
-  return r;
-}
-__device__ __forceinline__ void expand(const Raw<u16> &r, float (&x)[kVec]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x[2 * j] = __builtin_bit_cast(float, r.w[0][j] << 16);
-    x[2 * j + 1] = __builtin_bit_cast(float, r.w[0][j] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void expand(const Raw<float> &r, float (&x)[kVec]) {
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) {
-    const uint32_t w = r.w[j / 4][j % 4];  // (a copy: a bit cast of the vector's element itself reads element 0)
-    x[j] = __builtin_bit_cast(float, w);
-  }
-}
-// What is written here is read by another kernel, if at all soon by other XCDs:
-// streaming stores keep it out of the L2's way (65,536 rows loaded from 4 bits:
-// 33 us against 49 us with ordinary stores).
-__device__ __forceinline__ void st16_stream(void *p, u32x4 v) {
-  __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
-}
-// Eight of a lane's elements.  fp32: either store writes 16 bytes of every 32, which
-// reach memory in parts, so where four lanes hold 32 dims side by side (gap 0) they
-// trade first and a store writes 64 bytes side by side (16,384 rows of 16 heads of
-// 80 of which 40 dims turn: 46 us, 36 us so); otherwise the second four go `gap`
-// elements on.
-__device__ __forceinline__ void store_words(u16 *p, const u32x4 (&w)[1], int) { st16_stream(p, w[0]); }
-__device__ __forceinline__ void store_words(float *p, const u32x4 (&w)[2], int gap) {
-  if (gap) {
-    st16_stream(p, w[0]);
-    st16_stream(p + gap, w[1]);
-    return;
-  }
-  const int l = threadIdx.x & 3;
-  u32x4 a, b;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t x = w[0][j], y = w[1][j];
-    const uint32_t xa = dpp_mov<kDppQuad0011>(0u, x), ya = dpp_mov<kDppQuad0011>(0u, y);
-    const uint32_t xb = dpp_mov<kDppQuad2233>(0u, x), yb = dpp_mov<kDppQuad2233>(0u, y);
-    a[j] = l & 1 ? ya : xa;
-    b[j] = l & 1 ? yb : xb;
-  }
-  st16_stream(p - 4 * l, a);
-  st16_stream(p - 4 * l + 16, b);
-}
-template <typename T>
-__device__ __forceinline__ void store_raw(T *p, const Raw<T> &r, int gap) {
-  store_words(p, r.w, gap);
-}
-__device__ __forceinline__ void store(u16 *p, const float (&x)[kVec], int gap) {
-  u32x4 r[1];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bf16x2 b = {static_cast<__bf16>(x[2 * j]), static_cast<__bf16>(x[2 * j + 1])};
-    r[0][j] = __builtin_bit_cast(uint32_t, b);
-  }
-  store_words(p, r, gap);
-}
-__device__ __forceinline__ void store(float *p, const float (&x)[kVec], int gap) {
-  const u32x4 r[2] = {__builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}),
-                      __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]})};
-  store_words(p, r, gap);
-}
-__device__ __forceinline__ float one(const u16 *p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ float one(const float *p) { return *p; }
-
-// A result in fp32, kept as such: the compiler must not merge this rounding with
-// the one to bf16 that follows (two roundings and one differ near ties).
-__device__ __forceinline__ float to_f32(double x) {
-  float r = (float)x;
-  asm("" : "+v"(r));
-  return r;
-}
 
 // The turn, in place.  x[0] holds dims [o, o + 8) of a head, cs the row's cosines
 // and sines.  FULL: x[1] holds their partners, dims [o + half, o + half + 8), and
@@ -224,6 +103,17 @@ __device__ __forceinline__ void unpack(uint32_t codes, int scale, float (&x)[kVe
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2);
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3);
   const bf16x2 r[4] = {a, b, c, d};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[2 * j] = (float)r[j][0], x[2 * j + 1] = (float)r[j][1];
+}
+
+// The same of an 8-bit row: two dwords of codes and their block's scale byte.
+__device__ __forceinline__ void unpack(uint2 codes, int scale, float (&x)[kVec]) {
+  const float s = byte_scale(scale);
+  const bf16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.x, s, false),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.x, s, true),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.y, s, false),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.y, s, true)};
 #pragma unroll
   for (int j = 0; j < 4; ++j) x[2 * j] = (float)r[j][0], x[2 * j + 1] = (float)r[j][1];
 }
@@ -327,7 +217,9 @@ __global__ __launch_bounds__(kThreads, K == 1                                   
                                        : MODE == kRowAppend && SHAPE == kVectors && sizeof(T) == 2 ? 6
                                                                                                    : 1)
 void rows_kernel(RowParams p) {
-  constexpr bool kToKv = MODE == kRowAppend || MODE == kRowLoadMx, kMx = MODE == kRowAppendMx || MODE == kRowLoadMx;
+  constexpr bool kByte = MODE == kRowLoadByte, kLoad = MODE == kRowLoadMx || kByte;
+  constexpr bool kToKv = MODE == kRowAppend || kLoad, kMx = MODE == kRowAppendMx || kLoad;
+  using Codes = std::conditional_t<kByte, uint2, uint32_t>;  // of 8 dims
   constexpr bool kFull = SHAPE == kPairs;
   constexpr int NV = kFull ? 2 : 1;  // vectors of 8 dims of a lane
   // K = 1: at most 64 / lanes rows of 4 * NV * lanes frequencies each, with two heads
@@ -366,7 +258,7 @@ void rows_kernel(RowParams p) {
     int32_t at, from, page, mx_page;
     bool live;
     Raw<T> x[NV], y, v[NV];
-    uint32_t xc[NV], yc, vc[NV];  // 4-bit rows
+    Codes xc[NV], yc, vc[NV];  // 4-bit and 8-bit rows
     int32_t xs[NV], ys, vs[NV];
   };
   In in[K];
@@ -378,9 +270,9 @@ void rows_kernel(RowParams p) {
     c.unit = unit0 + u - r * units;
     if constexpr (MODE != kRowTurn) {
       c.at = c.from = p.pos[c.row];
-      if constexpr (MODE == kRowLoadMx) c.from = p.src_pos[c.row];
+      if constexpr (kLoad) c.from = p.src_pos[c.row];
     }
-    if constexpr (MODE != kRowLoadMx) {
+    if constexpr (!kLoad) {
       const bool query = MODE == kRowTurn || c.unit < p.n_q_heads;
       const int h = query ? c.unit : c.unit - p.n_q_heads;
       const T *src =
@@ -411,22 +303,28 @@ void rows_kernel(RowParams p) {
         if (p.pages.table) c.page = p.pages.table[c.at >> p.pages.shift];
       if constexpr (kMx) c.mx_page = mx_page(p.mx, c.row / p.mx.rows_per_seq, c.from);
     }
-    if constexpr (MODE == kRowLoadMx) {
+    if constexpr (kLoad) {
       const int64_t slot = ((int64_t)c.unit << p.mx.shift) + (c.from & ((1 << p.mx.shift) - 1));
-      const int64_t co = c.mx_page * p.mx.code_stride + slot * (D / 2);
-      const int64_t so = c.mx_page * p.mx.scale_stride + slot * (D / kMxBlock);
+      const int64_t co = c.mx_page * p.mx.code_stride + slot * (kByte ? D : D / 2);
+      const int64_t so = c.mx_page * p.mx.scale_stride + (kByte ? slot / kByteBlock : slot * (D / kMxBlock));
+      auto codes = [&](const uint8_t *pool, int d) __attribute__((always_inline)) {
+        return *reinterpret_cast<const Codes *>(pool + co + (kByte ? d : d / 2));
+      };
+      auto scale = [&](const uint8_t *pool, int d) __attribute__((always_inline)) {
+        return pool[so + (kByte ? 0 : d / kMxBlock)];
+      };
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        c.xc[i] = *reinterpret_cast<const uint32_t *>(p.mx.k + co + dims(i) / 2);
-        c.vc[i] = *reinterpret_cast<const uint32_t *>(p.mx.v + co + dims(i) / 2);
-        c.xs[i] = p.mx.k_scale[so + dims(i) / kMxBlock];
-        c.vs[i] = p.mx.v_scale[so + dims(i) / kMxBlock];
+        c.xc[i] = codes(p.mx.k, dims(i));
+        c.vc[i] = codes(p.mx.v, dims(i));
+        c.xs[i] = scale(p.mx.k_scale, dims(i));
+        c.vs[i] = scale(p.mx.v_scale, dims(i));
       }
       c.yc = c.xc[0];
       c.ys = c.xs[0];
       if (partners) {
-        c.yc = *reinterpret_cast<const uint32_t *>(p.mx.k + co + partner / 2);
-        c.ys = p.mx.k_scale[so + partner / kMxBlock];
+        c.yc = codes(p.mx.k, partner);
+        c.ys = scale(p.mx.k_scale, partner);
       }
     }
   }
@@ -457,7 +355,7 @@ void rows_kernel(RowParams p) {
     if (sub >= heads || k * heads + sub > last) return;
     const f64x2 *rcs = cs + (c.row - row0) * half;
     float x[NV][kVec], y[kVec], v[NV][kVec];
-    if constexpr (MODE == kRowLoadMx) {
+    if constexpr (kLoad) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         unpack(c.xc[i], c.xs[i], x[i]);
@@ -583,7 +481,8 @@ void launch_mode(const RowParams &p, RowMode mode, dim3 grid, hipStream_t s) {
     else if (mode == kRowAppendMx)
       rows_kernel<T, kRowAppendMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
     else if constexpr (SHAPE == kVectors || sizeof(T) == 2)
-      rows_kernel<T, kRowLoadMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
+      mode == kRowLoadMx ? rows_kernel<T, kRowLoadMx, K, SHAPE><<<grid, kThreads, 0, s>>>(p)
+                         : rows_kernel<T, kRowLoadByte, K, SHAPE><<<grid, kThreads, 0, s>>>(p);
   }
 }
 
@@ -600,13 +499,13 @@ void launch_shape(const RowParams &p, RowMode mode, HeadShape shape, dim3 grid, 
 }  // namespace
 
 hipError_t launch_rows(const RowParams &p, RowMode mode, bool bf16, hipStream_t s) {
-  static const char *const names[] = {"rotary", "append", "append_mx", "load_mx"};
+  static const char *const names[] = {"rotary", "append", "append_mx", "load_mx", "load_byte"};
   ProfScope ps(names[mode], s);
   const int half = p.rope.half;
   const int units = p.n_q_heads + p.n_kv_heads;
   // (fp32 rows loaded from 4 bits: 8 dims a lane let four lanes trade pieces of one
   // run of dims instead of two; 65,536 rows 58 us, in pairs 71)
-  const bool pairs = 2 * half == p.head_dim && units > 1 && (bf16 || mode != kRowLoadMx);
+  const bool pairs = 2 * half == p.head_dim && units > 1 && (bf16 || (mode != kRowLoadMx && mode != kRowLoadByte));
   const HeadShape shape = p.rope.adjacent || !half ? kVectors
                           : half % kVec           ? kSingles
                           : pairs                 ? kPairs
