@@ -1,5 +1,7 @@
 // Causal attention over the 8-bit KV cache, gfx950.
 //
+#include <type_traits>
+
 #include "attn_steps.h"
 
 namespace conduit {
@@ -100,7 +102,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
 
   while (part.t < part.t_end) {
     const Segment sg = shared ? segment_at(p, n_sb, s_prefix, part)
-                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0};
+                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0, 0};
     const int sb = sg.sb, h = sg.h, first = sg.first;
     int last = sg.last;
     const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
@@ -328,6 +330,387 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
   }
 }
 
+// Many pairs per KV head: keys and values are decoded once for 256 pairs into LDS.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+constexpr int kManyWaves = 8;
+constexpr int kManyThreads = 64 * kManyWaves;
+constexpr int kBytePairs = 32 * kManyWaves;          // pairs of a block
+constexpr int kManyPad = 3;                          // what beginning a block costs, in tiles
+constexpr int kRing = 4;                             // tiles in LDS
+constexpr float kHead = 11.f, kManySlack = 4.f;      // weights stay below 2^(kHead + kManySlack)
+constexpr float kFar = 89.f;
+
+__device__ __forceinline__ u32x4 half8(uint32_t lo, uint32_t hi) {
+  const f16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true)};
+  return __builtin_bit_cast(u32x4, r);
+}
+
+template <int D>
+__global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnParams p) {
+  constexpr int kPairs = kBytePairs;
+  constexpr int C = D / 16, DT = D / 32;
+  static_assert(C == 2 * DT, "as many products for scores as for outputs");
+  constexpr int KP = D + 8, VP = D + 16;
+  constexpr int LPK = D / 16;                          // 16-byte chunks of a key's codes
+  constexpr int kChunks = kTileKeys * LPK;             // of a tile, one a thread
+  __shared__ __attribute__((aligned(16))) u16 s_k[kRing][kTileKeys * KP];
+  __shared__ __attribute__((aligned(16))) u16 s_v[kRing][kTileKeys * VP];
+  __shared__ int s_sum[kManyWaves], s_least[kManyWaves];
+  extern __shared__ int s_prefix[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hh = lane >> 5;
+  const int hkv = p.mx.n_kv_heads, r = p.mx.rows_per_seq, G = p.group;
+  const int n_sb = p.n_seqs * p.blocks_per_seq;
+  Part part{0, 1, 0, 0, 0, 0};
+  if (p.n_workers && !plan_part<kManyWaves, 32, kManyPad>(p, kPairs, kTileKeys, s_sum, s_prefix, part)) return;
+  const int part0 = part.t;
+  const MxCache &c = p.mx;
+  const int v_lane = v_operand_lane_offset_il<VP>(lane);
+  const int k_lane = col * KP + 8 * hh;
+
+  while (part.t < part.t_end) {
+    const Segment sg = p.n_workers ? segment_at<kManyPad>(p, n_sb, s_prefix, part)
+                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0, 0};
+    part.t += sg.listed;
+    if (p.n_workers && sg.first == sg.last) continue;
+    const int seq = sg.sb / p.blocks_per_seq, rb = sg.sb - seq * p.blocks_per_seq, h = sg.h;
+    const int block0 = rb * kPairs, n_pairs = min(kPairs, r * G - block0);
+    const int64_t row_base = (int64_t)seq * r;
+
+    // A thread's chunk of a tile's codes in registers, on its way into LDS.
+    struct Raw {
+      u32x4 k, v;
+      int ks;
+      uint32_t vs;  // the value scales of the tile's four blocks
+    };
+    const SeqPages pages = seq_pages(c, seq);
+    const int64_t head = (int64_t)h << c.shift;
+    const int limit = min(sg.last, (c.n_ctx + kTileKeys - 1) / kTileKeys);  // no tile from here on is read
+    auto index = [&](int tile) __attribute__((always_inline)) { return min(tile, limit - 1) * kTileKeys >> c.shift; };
+    // Where a tile begins: in the code pools and in the scale pools.
+    struct Place {
+      int64_t codes, scales;
+    };
+    auto place = [&](int tile, int entry) __attribute__((always_inline)) {
+      const int64_t page = page_number(c, pages, index(tile), entry);
+      const int64_t slot = head + ((min(tile, limit - 1) * kTileKeys) & ((1 << c.shift) - 1));
+      return Place{page * c.code_stride + slot * D, page * c.scale_stride + slot / kByteBlock};
+    };
+    // (at head_dim 64 half of the threads)
+    const uint32_t chunk = kChunks == kManyThreads ? tid : min(tid, kChunks - 1);
+    const uint32_t lane_codes = chunk * 16, lane_scale = chunk / LPK / kByteBlock;
+    auto load_keys = [&](const Place &at, Raw &x) __attribute__((always_inline)) {
+      x.k = ld16(c.k + at.codes + lane_codes);
+      x.ks = (c.k_scale + at.scales)[lane_scale];
+    };
+    auto load_values = [&](const Place &at, Raw &x) __attribute__((always_inline)) {
+      x.v = ld16(c.v + at.codes + lane_codes);
+      int zero = 0;
+      asm("" : "+v"(zero));
+      x.vs = *reinterpret_cast<const uint32_t *>(c.v_scale + at.scales + zero);
+    };
+    // The first two tiles are on their way before anything else is.
+    Raw raw0, raw;
+    Place at2;
+    int entry3;
+    {
+      int entry[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) entry[i] = page_entry(pages, index(sg.first + i));
+      entry3 = page_entry(pages, index(sg.first + 3));
+      const Place at0 = place(sg.first, entry[0]), at1 = place(sg.first + 1, entry[1]);
+      at2 = place(sg.first + 2, entry[2]);
+      load_keys(at0, raw0);
+      load_values(at0, raw0);
+      load_keys(at1, raw);
+      load_values(at1, raw);
+    }
+
+    // The lane's pair: its query and how many keys it sees (one that is not there sees all).
+    const int j0 = 32 * wave + col, pair = block0 + j0;
+    bf16x8 q[C];
+    int seen = INT32_MAX, most = 0;
+#pragma unroll
+    for (int x = 0; x < C; ++x) q[x] = bf16x8{};
+    if (j0 < n_pairs) {
+      const int row = pair / G;
+      seen = most = keys_seen(p.pos[row_base + row], c.n_ctx);
+      const u16 *at =
+          static_cast<const u16 *>(p.q) + ((row_base + row) * p.n_q_heads + h * G + pair % G) * D + 8 * hh;
+#pragma unroll
+      for (int x = 0; x < C; ++x) q[x] = as_bf16x8(ld16(at + 16 * x));
+    }
+    most = __builtin_amdgcn_readfirstlane(wave_max_i(most));
+    const int least = __builtin_amdgcn_readfirstlane(wave_min_i(seen));
+    __syncthreads();
+    if (lane == 0) {
+      s_sum[wave] = most;
+      s_least[wave] = least;
+    }
+    __syncthreads();
+    int block_most = 0, block_least = INT32_MAX;
+    for (int w = 0; w < kManyWaves; ++w) {
+      block_most = max(block_most, s_sum[w]);
+      block_least = min(block_least, s_least[w]);
+    }
+    block_most = __builtin_amdgcn_readfirstlane(block_most);
+    block_least = __builtin_amdgcn_readfirstlane(block_least);
+    const int last = min(sg.last, (block_most + kTileKeys - 1) / kTileKeys);
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x16{};
+    // The running maximum of the pair's scores x, that of x + log2 of the value scale, and what
+    // follows from them.
+    float m, M, m_high, M_high, m_far, M_head, l = 0.f;
+    auto set_maxima = [&](float x, float y) __attribute__((always_inline)) {
+      m = x;
+      M = y;
+      m_high = x + kManySlack;
+      M_high = y + kManySlack;
+      m_far = x + kFar;
+      M_head = y - kHead;
+    };
+    set_maxima(kMInit, kMInit);
+
+    const int put_key = chunk / LPK, put_dim = chunk % LPK * 16;
+    const int k_put = put_key * KP + put_dim;
+    const int v_put =
+        ((put_key & ~15) + 8 * ((put_key >> 2) & 1) + 2 * (put_key & 3) + ((put_key >> 3) & 1)) * VP + put_dim;
+    const bool puts = kChunks == kManyThreads || tid < kChunks;
+    auto put_keys = [&](int tile, const Raw &x) __attribute__((always_inline)) {
+      u16 *dst = s_k[tile & (kRing - 1)] + k_put;
+      if (puts) {
+        st16(dst, __builtin_bit_cast(u32x4, unpack8(x.k[0], x.k[1], byte_scale(x.ks))));
+        st16(dst + 8, __builtin_bit_cast(u32x4, unpack8(x.k[2], x.k[3], byte_scale(x.ks))));
+      }
+    };
+    auto put_values = [&](int tile, const Raw &x) __attribute__((always_inline)) {
+      u16 *dst = s_v[tile & (kRing - 1)] + v_put;
+      if (puts) {
+        st16(dst, half8(x.v[0], x.v[1]));
+        st16(dst + 8, half8(x.v[2], x.v[3]));
+      }
+    };
+    auto clean = [&](int tile, Raw &x) __attribute__((always_inline)) {
+      if ((tile + 1) * kTileKeys > block_least) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x.v[y] = without_nan(x.v[y]);
+      }
+    };
+
+    // Scores of 32 keys, and for their softmax: whether the maxima rise in some lane, and the
+    // exponents that the two blocks' weights are over.
+    struct Scores {
+      f32x16 s;
+      float top[2], at[2];
+      uint64_t rises;
+    };
+    auto top_of = [&](Scores &x, int b) __attribute__((always_inline)) {
+      float t = kNegInf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t = fmaxf(t, x.s[8 * b + i]);
+      x.top[b] = t;
+    };
+    // (scale > 0)
+    auto largest = [&](const Scores &x, const float (&sv)[2], float &mx, float &my) __attribute__((always_inline)) {
+      mx = fmaxf(x.top[0], x.top[1]) * p.scale_log2;
+      my = fmaxf(__builtin_fmaf(x.top[0], p.scale_log2, sv[0]), __builtin_fmaf(x.top[1], p.scale_log2, sv[1]));
+    };
+    auto compare = [&](Scores &x, const float (&sv)[2]) __attribute__((always_inline)) {
+      float mx, my;
+      largest(x, sv, mx, my);
+      x.rises = __builtin_amdgcn_ballot_w64(mx > m_high) | __builtin_amdgcn_ballot_w64(my > M_high);
+    };
+    auto exponents = [&](Scores &x, const float (&sv)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) x.at[b] = fminf(M_head - sv[b], m_far);
+    };
+    // Keys that a row does not see, and maxima that rise: sums and outputs follow.
+    auto settle = [&](Scores &x, int key0, const float (&sv)[2]) __attribute__((always_inline)) {
+      if (key0 + 32 > least) {
+        const int limit = seen - key0 - 4 * hh;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.s[i] = (i & 3) + 8 * (i >> 2) < limit ? x.s[i] : kNegInf;
+        top_of(x, 0);
+        top_of(x, 1);
+        compare(x, sv);
+      }
+      if (x.rises) {
+        float mx, my;
+        largest(x, sv, mx, my);
+        const float mn = fmaxf(m, half_max(mx)), Mn = fmaxf(M, half_max(my));
+        l *= fast_exp2(m - mn);
+        const float a = fast_exp2(M - Mn);
+        set_maxima(mn, Mn);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= a;
+        exponents(x, sv);
+      }
+    };
+    auto scale_of_step = [&](uint32_t vs, int half, float (&sv)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        sv[b] = (float)(min(max((int)(vs >> (16 * half + 8 * b) & 0xff), kByteScaleMin), kByteScaleMax) - 127);
+    };
+
+    if (sg.first < last) {
+      uint32_t vs0, vs1, vs2;  // value scales of this tile and the next two
+      clean(sg.first, raw0);
+      put_keys(sg.first, raw0);
+      put_values(sg.first, raw0);
+      vs0 = __builtin_amdgcn_readfirstlane(raw0.vs);
+      clean(sg.first + 1, raw);
+      put_keys(sg.first + 1, raw);
+      put_values(sg.first + 1, raw);
+      vs1 = __builtin_amdgcn_readfirstlane(raw.vs);
+      load_keys(at2, raw);
+      load_values(at2, raw);
+      __syncthreads();
+      u32x4 ring[C];  // operands: a step's keys, then its values
+      auto key_operand = [&](int step, int x) __attribute__((always_inline)) {
+        return ld16(s_k[(step >> 1) & (kRing - 1)] + 32 * (step & 1) * KP + k_lane + 16 * x);
+      };
+      auto value_operand = [&](int step, int x) __attribute__((always_inline)) {
+        return __builtin_bit_cast(u32x4, v_operand_il<VP>(s_v[(step >> 1) & (kRing - 1)] + 32 * (step & 1) * VP +
+                                                          v_lane + 16 * (x / DT) * VP + 32 * (x % DT)));
+      };
+      Scores xa, xb;
+      float sv0[2], sv1[2];  // value scales (log2) of this step's blocks and of the next one's
+      const int step0 = 2 * sg.first;
+      xa.s = f32x16{};
+#pragma unroll
+      for (int x = 0; x < C; ++x)
+        xa.s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(key_operand(step0, x)), q[x], xa.s, 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < C; ++x) ring[x] = key_operand(step0 + 1, x);
+      scale_of_step(vs0, 0, sv0);
+      top_of(xa, 0);
+      top_of(xa, 1);
+      compare(xa, sv0);
+      exponents(xa, sv0);
+      settle(xa, 32 * step0, sv0);
+      // One step: the softmax of its scores x beside the products of the next scores y, then the
+      // outputs' products beside what follows from y.  Slots hold one product and its share of the
+      // vector work each: what a slot computes stays there (the empty statements).
+      auto step = [&](int s, Scores &x, Scores &y, const float (&svn)[2], auto &&extra) __attribute__((always_inline)) {
+        constexpr int kPer = 16 / C;
+        float back[2], sum[2] = {0.f, 0.f}, e[16];
+        f16x8 pr[2];
+        auto finish = [&](int i) __attribute__((always_inline)) {
+          sum[i >> 3] = (i & 7) ? sum[i >> 3] + e[i] : e[i];
+          asm volatile("" ::"v"(sum[i >> 3]));
+          if (i & 1) {
+            const f16x2 w = {(_Float16)e[i - 1], (_Float16)e[i]};
+            const uint32_t u = __builtin_bit_cast(uint32_t, w);
+            asm volatile("" ::"v"(u));
+            u32x4 z = __builtin_bit_cast(u32x4, pr[i >> 3]);
+            z[(i & 7) >> 1] = u;
+            pr[i >> 3] = __builtin_bit_cast(f16x8, z);
+          }
+        };
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+          y.s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ring[j]), q[j], j == 0 ? f32x16{} : y.s, 0, 0, 0);
+          ring[j] = value_operand(s, j);
+#pragma unroll
+          for (int i = kPer * j; i < kPer * (j + 1); ++i) {
+            e[i] = fast_exp2(__builtin_fmaf(x.s[i], p.scale_log2, -x.at[i >> 3]));
+            asm volatile("" ::"v"(e[i]));
+            if (i > 0) finish(i - 1);
+          }
+          if (j == 1 || j == 2) {
+            back[j - 1] = fast_exp2(x.at[j - 1] - m);
+            asm volatile("" ::"v"(back[j - 1]));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+          if (j == 0) finish(15);
+          o[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, ring[j]), pr[j / DT], o[j % DT],
+                                                             0, 0, 0);
+          ring[j] = key_operand(s + 2, j);
+          if (j == 0) {
+            l = __builtin_fmaf(sum[1], back[1], __builtin_fmaf(sum[0], back[0], l));
+            asm volatile("" ::"v"(l));
+          }
+          extra(j);
+          if (j == C - 3 || j == C - 2) {
+            top_of(y, j - (C - 3));
+            asm volatile("" ::"v"(y.top[j - (C - 3)]));
+          }
+          if (j == C - 1) {
+            compare(y, svn);
+            exponents(y, svn);
+            asm volatile("" ::"v"(y.at[0]), "v"(y.at[1]), "s"(y.rises));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        settle(y, 32 * s + 32, svn);
+      };
+      // (a wave whose rows end before the block's goes on: masked, and rarely by more than
+      // a few tiles)
+      for (int tile = sg.first; tile < last; ++tile) {
+        clean(tile + 2, raw);
+        scale_of_step(vs0, 1, sv1);
+        // Registers are loaded anew once they are in LDS: a tile ahead of their use.
+        Place at3;
+        step(2 * tile, xa, xb, sv1, [&](int j) __attribute__((always_inline)) {
+          if (j == 0) put_keys(tile + 2, raw);
+          if (j == 1) at3 = place(tile + 3, entry3);
+          if (j == 2) load_keys(at3, raw);
+        });
+        scale_of_step(vs1, 0, sv0);
+        step(2 * tile + 1, xb, xa, sv0, [&](int j) __attribute__((always_inline)) {
+          if (j == 0) {
+            put_values(tile + 2, raw);
+            vs2 = __builtin_amdgcn_readfirstlane(raw.vs);
+          }
+          if (j == 1) load_values(at3, raw);
+          if (j == 2) entry3 = page_entry(pages, index(tile + 4));
+        });
+        vs0 = vs1;
+        vs1 = vs2;
+        __syncthreads();
+      }
+    }
+
+    const bool whole = !p.n_workers || (sg.first == 0 && sg.last == sg.steps);
+    const int slot = 2 * blockIdx.x + (part.t - sg.listed == part0 ? 0 : 1);
+    l += __shfl_xor(l, 32, 64);
+    if (j0 < n_pairs) {
+      const int64_t gp = (row_base + pair / G) * p.n_q_heads + h * G + pair % G;
+      const float unit = fast_exp2(M - m - kHead), inv = l == 0.f ? 0.f : unit / l;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 32 * dt + 8 * i + 4 * hh;
+          const f32x4 y = {o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+          if (whole)
+            *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
+                make_ushort4(f32_to_bf16(y[0] * inv), f32_to_bf16(y[1] * inv), f32_to_bf16(y[2] * inv),
+                             f32_to_bf16(y[3] * inv));
+          else
+            *reinterpret_cast<f32x4 *>(p.part_o + ((int64_t)slot * kPairs + j0) * D + e) = y * unit;
+        }
+      if (hh == 0) {
+        if (!whole)
+          p.part_ml[(int64_t)slot * kPairs + j0] = make_float2(m, l);
+        else if (p.lse_out)
+          p.lse_out[gp] = l == 0.f ? kNegInf : (m + __log2f(l)) * kLn2;
+      }
+    }
+    if (!p.n_workers) break;
+  }
+}
+
 template <int D, int W>
 void launch_few(const MxAttnParams &p, bool wide, bool bf16, int grid, size_t lds, hipStream_t s) {
   if (bf16)
@@ -344,7 +727,9 @@ void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStre
   const int n_sb = p.n_seqs * p.blocks_per_seq;
   const int grid = p.n_workers ? p.n_workers : n_sb * p.mx.n_kv_heads;
   const size_t lds = p.n_workers && n_sb > kLaneBlocks ? (size_t)(n_sb + 1) * 4 : 0;
-  if (p.n_workers || grid > 256)
+  if (sh.pairs == kBytePairs)
+    attn_byte_many_kernel<D><<<grid, kManyThreads, lds, s>>>(p);
+  else if (p.n_workers || grid > 256)
     launch_few<D, 4>(p, sh.pairs > 16, bf16, grid, lds, s);
   else
     launch_few<D, 8>(p, sh.pairs > 16, bf16, grid, lds, s);
@@ -356,12 +741,13 @@ MxAttnShape byte_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_he
                           int32_t head_dim, bool bf16) {
   MxAttnShape L{};
   const int64_t pairs = (int64_t)rows_per_seq * (n_q_heads / n_kv_heads);
-  L.pairs = few_pairs(head_dim, pairs, bf16);
+  const bool many = bf16 && pairs > 32;
+  L.pairs = many ? kBytePairs : few_pairs(head_dim, pairs, bf16);
   L.blocks_per_seq = (int32_t)((pairs + L.pairs - 1) / L.pairs);
   const int64_t n_sb = (int64_t)n_seqs * L.blocks_per_seq, blocks = n_sb * n_kv_heads;
   const int64_t steps = ((int64_t)n_ctx + kStep - 1) / kStep;
   const int64_t resident =
-      256 * waves_per_simd(head_dim, L.pairs > 16 ? 2 : 1, bf16 ? 1 : 3);
+      256 * (many ? 1 : waves_per_simd(head_dim, L.pairs > 16 ? 2 : 1, bf16 ? 1 : 3));
   // Workgroups share the steps out evenly, for a second launch that merges, from
   // this many steps of a block on (and while the parts' list fits LDS): fewer are
   // done sooner by a workgroup per block, and the more blocks there are the less
@@ -370,7 +756,7 @@ MxAttnShape byte_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_he
   // us.  256 of up to 4,096: 75 and 84 us, of up to 8,192: 144 and 140 us.
   const int64_t from = blocks < 256 ? 8 : blocks < 1024 ? 16 : 32;
   // (The merge has up to L.pairs workgroups of 256 threads a block, fewer than 2^32.)
-  if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * steps < INT32_MAX &&
+  if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * (steps + kManyPad) < INT32_MAX &&
       blocks * L.pairs < 1 << 24)
     L.n_workers = (int32_t)std::min<int64_t>(resident, std::max<int64_t>(1, blocks * steps / kMinSteps));
   lay_out_workspace(L, n_sb, head_dim);
@@ -384,7 +770,7 @@ hipError_t launch_attn_byte(const MxAttnParams &p, const MxAttnShape &sh, int he
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.n_workers) return e;
-  return launch_attn_merge(p, sh, "attn_byte_merge", head_dim, bf16, s);
+  return launch_attn_merge(p, sh, "attn_byte_merge", head_dim, bf16, s, sh.pairs == kBytePairs ? kManyPad : 0);
 }
 
 }  // namespace conduit

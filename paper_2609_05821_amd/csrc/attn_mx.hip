@@ -145,7 +145,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_mx_ker
 
   while (part.t < part.t_end) {
     const Segment sg = shared ? segment_at(p, n_sb, s_prefix, part)
-                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0};
+                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0, 0};
     const int sb = sg.sb, h = sg.h, first = sg.first;
     int last = sg.last;
     const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_mx_many_kernel(MxAttnParams 
 
   while (part.t < part.t_end) {
     const Segment sg = p.n_workers ? segment_at(p, n_sb, s_prefix, part)
-                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0};
+                                   : Segment{(int)blockIdx.x / hkv, (int)blockIdx.x % hkv, 0, INT32_MAX, 0, 0};
     const int seq = sg.sb / p.blocks_per_seq, rb = sg.sb - seq * p.blocks_per_seq, h = sg.h;
     const int block0 = rb * kPairs, n_pairs = min(kPairs, r * G - block0);
     const int64_t row_base = (int64_t)seq * r;

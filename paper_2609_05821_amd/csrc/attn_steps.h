@@ -71,18 +71,19 @@ __device__ __forceinline__ int wave_min_i(int x) {
 __device__ __forceinline__ int keys_seen(int pos, int n_ctx) { return min(max(pos, -1), n_ctx - 1) + 1; }
 
 // Steps of `step` keys of sequence block sb for one KV head (positions loaded
-// eight at a time).
+// BATCH at a time).
+template <int BATCH>
 __device__ __forceinline__ int block_steps(const MxAttnParams &p, int sb, int pairs, int step) {
   const int s = sb / p.blocks_per_seq, rb = sb - s * p.blocks_per_seq, r = p.mx.rows_per_seq;
   const int lo = rb * pairs / p.group, hi = min((rb * pairs + pairs - 1) / p.group, r - 1);
   const int32_t *pos = p.pos + (int64_t)s * r;
   int top = -1;
-  for (int i = lo; i <= hi; i += 8) {
-    int x[8];
+  for (int i = lo; i <= hi; i += BATCH) {
+    int x[BATCH];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = pos[min(i + j, hi)];
+    for (int j = 0; j < BATCH; ++j) x[j] = pos[min(i + j, hi)];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, x[j]);
+    for (int j = 0; j < BATCH; ++j) top = max(top, x[j]);
   }
   return (keys_seen(top, p.mx.n_ctx) + step - 1) / step;
 }
@@ -109,22 +110,33 @@ struct Part {
   int cut;
   int before, after, steps;  // up to kLaneBlocks: the lane's block in the list, and its steps per head
 };
+//
+// W: waves of the workgroup.  BATCH: see block_steps.  PAD: steps that a block is listed with
+// before its own, for what beginning it costs a workgroup (merge: the same).  With blocks of
+// many pairs, whose first products wait for queries, pages and a tile in LDS, a workgroup
+// that had ten short blocks ended long after one that had half of a long one.
+template <int W = kWaves, int BATCH = 8, int PAD = 0>
 __device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int step, int *s_sum, int *s_prefix,
                                           Part &part) {
+  constexpr int kWaves = W, kThreads = 64 * W;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n_sb = p.n_seqs * p.blocks_per_seq, hkv = p.mx.n_kv_heads, w = blockIdx.x;
   int total = 0;
   if (n_sb <= kLaneBlocks) {
-    part.steps = lane < n_sb ? block_steps(p, lane, pairs, step) : 0;
+    part.steps = lane < n_sb ? block_steps<BATCH>(p, lane, pairs, step) : 0;
     int own = part.steps * hkv;
+    int steps = 0;  // of the call, without PAD
+    if (PAD) steps = __builtin_amdgcn_readlane((int)wave_inclusive_sum((uint32_t)own), 63);
+    if (PAD && own) own += PAD * hkv;
     part.after = (int)wave_inclusive_sum((uint32_t)own);
     part.before = part.after - own;
     total = __builtin_amdgcn_readlane(part.after, 63);
+    if (!PAD) steps = total;
     if (w == 0 && wave == 0) {
       if (lane < n_sb) p.prefix[lane] = part.before;
       if (lane == 0) p.prefix[n_sb] = total;
     }
-    const int n = workers(p.n_workers, total), equal = max(1, (total + n - 1) / n);
+    const int n = workers(p.n_workers, steps), equal = max(1, (steps + n - 1) / n);
     for (int x = equal; x <= equal + kOver; ++x) {
       own = (part.steps + x - 1) / x * hkv;
       const int incl = (int)wave_inclusive_sum((uint32_t)own), all = __builtin_amdgcn_readlane(incl, 63);
@@ -145,7 +157,8 @@ __device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int 
   } else {
     for (int b0 = 0; b0 < n_sb; b0 += kThreads) {
       const int sb = b0 + tid;
-      const int own = sb < n_sb ? block_steps(p, sb, pairs, step) * hkv : 0;
+      int own = sb < n_sb ? block_steps<BATCH>(p, sb, pairs, step) * hkv : 0;
+      if (PAD && own) own += PAD * hkv;
       const int incl = (int)wave_inclusive_sum((uint32_t)own);
       __syncthreads();
       if (lane == 63) s_sum[wave] = incl;
@@ -172,10 +185,11 @@ __device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int 
 }
 
 // What of a part lies in one (sequence block, KV head): its steps [first, last)
-// of `steps`.
+// of `steps` (none where the part ends within PAD), and how far that goes in the list.
 struct Segment {
-  int sb, h, first, last, steps;
+  int sb, h, first, last, steps, listed;
 };
+template <int PAD = 0>
 __device__ __forceinline__ Segment segment_at(const MxAttnParams &p, int n_sb, const int *s_prefix, const Part &part) {
   int sb, begin, steps;
   if (n_sb <= kLaneBlocks) {
@@ -191,12 +205,18 @@ __device__ __forceinline__ Segment segment_at(const MxAttnParams &p, int n_sb, c
     }
     sb = __builtin_amdgcn_readfirstlane(lo);
     begin = __builtin_amdgcn_readfirstlane(s_prefix[lo]);
-    steps = __builtin_amdgcn_readfirstlane((s_prefix[lo + 1] - begin) / p.mx.n_kv_heads);
+    steps = __builtin_amdgcn_readfirstlane((s_prefix[lo + 1] - begin) / p.mx.n_kv_heads) - PAD;
+  }
+  if (PAD && !part.cut) {
+    const int h = (part.t - begin) / (steps + PAD), from = part.t - begin - h * (steps + PAD);
+    const int to = min(steps + PAD, from + part.t_end - part.t);
+    return {sb, h, max(from - PAD, 0), max(to - PAD, 0), steps, to - from};
   }
   const int per_head = part.cut ? (steps + part.cut - 1) / part.cut : steps, at = part.t - begin;
   const int h = at / per_head, rest = at - h * per_head;
   const int first = part.cut ? rest * part.cut : rest;
-  return {sb, h, first, min(steps, first + (part.cut ? part.cut : part.t_end - part.t)), steps};
+  const int last = min(steps, first + (part.cut ? part.cut : part.t_end - part.t));
+  return {sb, h, first, last, steps, part.cut ? 1 : last - first};
 }
 
 // Pages of one sequence, looked up in two parts: the block-table entry is loaded
@@ -231,7 +251,7 @@ __device__ __forceinline__ int page_number(const MxCache &c, const SeqPages &s, 
 // of blocks without keys.  A workgroup takes PW pairs of a block, a group of D / 4
 // lanes each; with PW = 1 all groups share the parts of one pair.
 template <int D, bool BF16, int PW>
-__global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int pairs) {
+__global__ __launch_bounds__(256) void attn_merge_kernel(MxAttnParams p, int pairs, int pad) {
   constexpr int L4 = D / 4;          // lanes of a part
   constexpr int kGroups = 256 / L4, kShare = kGroups / PW;
   // Parts a group has on their way at a time: where a workgroup shares one pair's,
@@ -250,7 +270,7 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int 
   if (rb * pairs + chunk * PW >= p.mx.rows_per_seq * p.group) return;
   const int base = p.prefix[sb], next = p.prefix[sb + 1], total = p.prefix[p.n_seqs * p.blocks_per_seq];
   const int cut = *p.cut;
-  const int n = workers(p.n_workers, total), steps = (next - base) / hkv;
+  const int n = workers(p.n_workers, total), steps = (next - base) / hkv;  // (with `pad`)
   float M = kMInit, L = 0.f;
   f32x4 o{};
   if (steps > 0) {
@@ -259,8 +279,9 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int 
     const int t0 = base + h * steps, t1 = t0 + steps;
     int w0 = (int)(((double)(t0 + 1) * n - 1) / total), w1 = (int)(((double)t1 * n - 1) / total);
     int first = 2 * w0 + (part_begin(w0, total, n) >= t0 ? 0 : 1);
+    while (pad && !cut && part_begin(w0 + 1, total, n) - t0 <= pad) first = 2 * ++w0;  // (has no step of its own)
     if (cut) {
-      const int parts = (steps + cut - 1) / cut;
+      const int parts = (steps - pad + cut - 1) / cut;
       w0 = p.parts[sb] + h * parts;
       w1 = w0 + parts - 1;
       first = 2 * w0;
@@ -324,14 +345,15 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnParams p, int 
 }
 
 template <int D, int PW>
-void launch_merge(const MxAttnParams &p, const MxAttnShape &sh, int blocks, bool few, bool bf16, hipStream_t s) {
+void launch_merge(const MxAttnParams &p, const MxAttnShape &sh, int pad, int blocks, bool few, bool bf16,
+                  hipStream_t s) {
   const int pairs = std::min(sh.pairs, p.mx.rows_per_seq * p.group);  // of the largest block
   const int grid = blocks * (few ? pairs : (pairs + PW - 1) / PW);
   if (few)
-    bf16 ? attn_mx_merge_kernel<D, true, 1><<<grid, 256, 0, s>>>(p, sh.pairs)
-         : attn_mx_merge_kernel<D, false, 1><<<grid, 256, 0, s>>>(p, sh.pairs);
+    bf16 ? attn_merge_kernel<D, true, 1><<<grid, 256, 0, s>>>(p, sh.pairs, pad)
+         : attn_merge_kernel<D, false, 1><<<grid, 256, 0, s>>>(p, sh.pairs, pad);
   else
-    attn_mx_merge_kernel<D, true, PW><<<grid, 256, 0, s>>>(p, sh.pairs);
+    attn_merge_kernel<D, true, PW><<<grid, 256, 0, s>>>(p, sh.pairs, pad);
 }
 
 // Workspace of a call whose workgroups share the steps.
@@ -351,14 +373,14 @@ inline void lay_out_workspace(MxAttnShape &L, int64_t n_sb, int head_dim) {
 // The launch that merges, where workgroups share the steps.  Few pairs: many parts of
 // each, shared out over a workgroup; many pairs: a few parts of each, one group of lanes.
 inline hipError_t launch_attn_merge(const MxAttnParams &p, const MxAttnShape &sh, const char *name, int head_dim,
-                                    bool bf16, hipStream_t s) {
+                                    bool bf16, hipStream_t s, int pad = 0) {
   ProfScope ps(name, s);
   const int blocks = p.n_seqs * p.blocks_per_seq * p.mx.n_kv_heads;
   const bool few = sh.pairs <= 32 || p.n_workers > 4 * blocks;
   if (head_dim == 128)
-    launch_merge<128, 8>(p, sh, blocks, few, bf16, s);
+    launch_merge<128, 8>(p, sh, pad, blocks, few, bf16, s);
   else
-    launch_merge<64, 16>(p, sh, blocks, few, bf16, s);
+    launch_merge<64, 16>(p, sh, pad, blocks, few, bf16, s);
   return hipGetLastError();
 }
 

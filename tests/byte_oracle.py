@@ -129,3 +129,23 @@ def attention_bounds(o, lse, av, mag, n_keys, d, bf16):
     bo = (es + (2.0 ** -12 if bf16 else 0.0))[..., None] * av + (2.0 ** -8 if bf16 else 2.0 ** -24) * o.abs() + 1e-30
     bl = es + 2.0 ** -21 * lse.abs().nan_to_num(0.0, 0.0, 0.0) + 2.0 ** -22
     return bo, bl
+
+
+def weight_floor(q, k, v, factors, pos, lse, scale=None):
+    """bf16 with many pairs: probabilities enter the product in fp16, as p_t f_t (f: the
+    factor of the block's scale) over 2^-11 times a power of two that is at most 2^4 below
+    and no more than the row's largest p_t f_t above it.  Below fp16's normal numbers a
+    weight is off by up to half its smallest step, 2^-25, so by 2^-36 max(p f): times the
+    codes, summed over the row's keys.  q [n, Hq, d], k, v [len, Hkv, d], factors [len, Hkv]."""
+    n, hq, d = q.shape
+    g = hq // k.shape[1]
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    codes = v.abs() / factors[..., None]
+    out = torch.zeros(n, hq, d, dtype=torch.float64)
+    for i in range(n):
+        m = min(int(pos[i]) + 1, k.shape[0])
+        if m > 0:
+            logits = (k[:m].repeat_interleave(g, 1) * q[i].double()).sum(-1) * scale        # [m, hq]
+            largest = (torch.exp(logits - lse[i]) * factors[:m].repeat_interleave(g, 1)).amax(0)
+            out[i] = 2.0 ** -36 * largest[:, None] * codes[:m].sum(0).repeat_interleave(g, 0)
+    return out

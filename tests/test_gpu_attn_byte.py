@@ -44,6 +44,11 @@ class Store:
         return tuple(B.decoded(self.cpu[i][pages, :, slot]) * B.factor(self.cpu[i + 2][pages, :, slot // 16])[..., None]
                      for i in (0, 1))
 
+    def factors(self, s, n):
+        """Factors of the value scales of tokens 0 .. n - 1 of sequence s."""
+        pos = torch.arange(n)
+        return B.factor(self.cpu[3][self.table[s, pos // self.page].long(), :, pos % self.page // 16])
+
     def set(self, which, s, t, value):
         """Every code of token t of sequence s in pool `which`, or the scales of its block."""
         slot = t % self.page
@@ -67,6 +72,8 @@ def check(st, q, pos, o, lse, scale=None, rows=None):
         qq = q[s * r:(s + 1) * r][list(sel)]
         want = M.attention(qq, k, v, p[list(sel)], scale)
         bo, bl = B.attention_bounds(*want, n, st.d, q.dtype == torch.bfloat16)
+        if q.dtype == torch.bfloat16 and r * st.hq // st.hkv > 32:
+            bo = bo + B.weight_floor(qq, k, v, st.factors(s, n), p[list(sel)], want[1], scale)
         go, gl = o[s * r:(s + 1) * r][list(sel)].double(), lse[s * r:(s + 1) * r][list(sel)].double()
         err = (go - want[0]).abs()
         assert (err <= bo).all(), f"sequence {s}: output {(err / bo).max():.3g} of the bound"
