@@ -668,8 +668,8 @@ typedef struct {
  *
  * pos       device int32 [n].  Within a sequence the positions in [0, n_ctx) ascend
  *           (a block that they come back to has meaningless contents); of rows with one
- *           position one is held.  A row whose position is outside leaves the cache as
- *           it was (padded rows: -1); its q_out is still written.
+ *           position the last is held.  A row whose position is outside leaves the cache
+ *           as it was (padded rows: -1); its q_out is still written.
  * n_held    nullable device int32 [n_seqs]: tokens that each sequence holds before the
  *           call, 0 .. n_held[s] - 1, are kept (values outside [0, n_ctx] are read as the
  *           nearest).  NULL, for rows behind all others: what a block has before the last
@@ -677,7 +677,8 @@ typedef struct {
  *           are free: their codes stay as they were while the scale may not.
  * k_out, v_out  nullable device [n][n_kv_heads][head_dim] dense, rows->dtype: the
  *           keys and values as the cache holds them (a row that pos leaves out: as in a
- *           block of its own).  May not overlap the rows.
+ *           block of its own; one whose position a later row has is not written).  May not
+ *           overlap the rows.
  * ------------------------------------------------------------------------ */
 conduit_status conduit_append_byte(const conduit_kv_byte *cache, const conduit_rows *rows, const int32_t *pos,
                                    const int32_t *n_held, const conduit_rope *rope, const int32_t *rope_pos,

@@ -1,9 +1,9 @@
 // New rows into the 8-bit cache, quantised as they are written, gfx950.
 //
 // 16 tokens and a head share a scale, so the unit of work is a run: the rows of a
-// call that go to one block of 16 tokens.  A wave takes a run's keys and values of one
+// call that go to one block of 16 tokens.  A wave takes a run's keys or values of one
 // head whole, 16 dims a lane and 16 tokens (2,048 elements at head_dim 128): their
-// largest magnitudes need no exchange beyond the wave, and the codes are written once.
+// largest magnitude needs no exchange beyond the wave, and the codes are written once.
 //   scale    s = the smallest with max|x| <= 448 2^(s - 127) over the rows written, and no
 //            less than the block's while it keeps other tokens.  A power of two: codes
 //            keep their 4 significant bits when it rises (but for those that fall below
@@ -22,12 +22,16 @@
 namespace conduit {
 namespace {
 
-constexpr int kMaxWaves = 4;  // heads of a run that a workgroup takes side by side
+// Heads of a run that a workgroup takes side by side, two waves each: one has the keys,
+// the other the values.
+constexpr int kMaxHeads = 4;
+constexpr int kMaxWaves = 2 * kMaxHeads;
 // Rows of a window: 1 keeps the chip busy with few rows (the rows that continue a
 // run leave at once), 16 saves those workgroups where there are many.
-constexpr int kWindow = 16;
-constexpr int kWindowFrom = 4096;
-constexpr int kQueryRows = 4;  // rows of a workgroup that turns queries (1 below kWindowFrom rows)
+constexpr int kWindow = 16, kWindowFew = 4;
+constexpr int kWindowFrom = 8192;
+// Rows of a workgroup that turns queries, and from how many rows on.
+constexpr int kQueryRows = 2, kQueryRowsFrom = 512;
 
 // A lane's 16 dims of a head: two vectors of 8, which turn together where they are
 // the two halves of pairs (t >= 0: the first of 8 frequencies).
@@ -52,6 +56,7 @@ __device__ __forceinline__ void turn(float (&x)[2][kVec], const LaneDims &d, int
       const double a = x[0][j], b = x[1][j];
       x[0][j] = to_f32(__builtin_fma(a, t[0], -(b * t[1])));
       x[1][j] = to_f32(__builtin_fma(b, t[0], a * t[1]));
+      __builtin_amdgcn_sched_barrier(0);  // (angles of one pair in registers at a time)
     }
   } else if (adjacent) {
 #pragma unroll
@@ -63,6 +68,7 @@ __device__ __forceinline__ void turn(float (&x)[2][kVec], const LaneDims &d, int
         const double a = x[i][2 * j], b = x[i][2 * j + 1];
         x[i][2 * j] = to_f32(__builtin_fma(a, t[0], -(b * t[1])));
         x[i][2 * j + 1] = to_f32(__builtin_fma(b, t[0], a * t[1]));
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -75,7 +81,7 @@ __device__ __forceinline__ f64x2 angle(const RopeTable &rope, int row, int f) {
 #pragma unroll
   for (int a = 0; a < 4; ++a) at[a] = a < rope.n_axes ? pos[a * rope.pos_stride] : 0;
   const int axis = rope.axis[f];
-  return cos_sin((double)(axis < 2 ? axis ? at[1] : at[0] : axis == 2 ? at[2] : at[3]) * (double)rope.inv_freq[f]);
+  return cos_sin<true>((double)(axis < 2 ? axis ? at[1] : at[0] : axis == 2 ? at[2] : at[3]) * (double)rope.inv_freq[f]);
 }
 
 // x as a cache of T would hold it.
@@ -138,53 +144,53 @@ __device__ __forceinline__ void decode8(uint2 c, float scale, float (&x)[kVec]) 
 // 2^e for -126 <= e <= 127.
 __device__ __forceinline__ float two_to(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
-// Queries of rows [row0, row0 + n): the workgroup's threads go over the heads' lanes.
+// Queries of rows [row0, row0 + n): the workgroup's threads go over the heads' lanes, the first
+// loads on their way before the angles are worked out.
 template <typename T, int D>
 __device__ __forceinline__ void turn_queries(const RowParams &p, int row0, int n, f64x2 *cs) {
   constexpr int LR = D / 16;
   const int half = p.rope.half, tid = threadIdx.x;
   const bool adjacent = p.rope.adjacent != 0;
+  const int items = n * p.n_q_heads * LR;
+  const LaneDims d = lane_dims<D>(tid % LR, half, adjacent);  // (the threads are a multiple of LR)
+  const int gap = half / kVec % 4 && !adjacent ? 4 : 0;
+  Raw<T> raw[2];
+  int row = 0, at = 0;
+  auto fetch = [&](int item) __attribute__((always_inline)) {
+    const int unit = min(item, items - 1) / LR;
+    row = unit / p.n_q_heads;
+    at = (unit - row * p.n_q_heads) * D;
+    const T *src = static_cast<const T *>(p.q) + (int64_t)(row0 + row) * p.q_stride + at;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) raw[i] = load_raw<T>(src + d.at[i]);
+  };
+  fetch(tid);
   for (int e = tid; e < n * half; e += blockDim.x) cs[e] = angle(p.rope, row0 + e / half, e % half);
   __syncthreads();
-  const int items = n * p.n_q_heads * LR;
-  const LaneDims d = lane_dims<D>(tid % LR, half, adjacent);  // (blockDim is a multiple of LR)
-  const int gap = half / kVec % 4 && !adjacent ? 4 : 0;
-  constexpr int K = 2;
-  for (int e0 = tid; e0 < items; e0 += K * blockDim.x) {
-    Raw<T> raw[K][2];
-    int row[K], at[K];
+  for (int e = tid; e < items;) {
+    float x[2][kVec];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int unit = min(e0 + k * (int)blockDim.x, items - LR + tid % LR) / LR;
-      row[k] = unit / p.n_q_heads;
-      at[k] = (unit - row[k] * p.n_q_heads) * D;
-      const T *src = static_cast<const T *>(p.q) + (int64_t)(row0 + row[k]) * p.q_stride + at[k];
+    for (int i = 0; i < 2; ++i) expand(raw[i], x[i]);
+    turn<D>(x, d, half, adjacent, cs + row * half);
+    T *dst = static_cast<T *>(p.q_out) + (int64_t)(row0 + row) * p.q_out_stride + at;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) raw[k][i] = load_raw<T>(src + d.at[i]);
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (e0 + k * (int)blockDim.x >= items) break;
-      float x[2][kVec];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) expand(raw[k][i], x[i]);
-      turn<D>(x, d, half, adjacent, cs + row[k] * half);
-      T *dst = static_cast<T *>(p.q_out) + (int64_t)(row0 + row[k]) * p.q_out_stride + at[k];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) store(dst + d.at[i], x[i], gap);
-    }
+    for (int i = 0; i < 2; ++i) store(dst + d.at[i], x[i], gap);
+    e += blockDim.x;
+    if (e < items) fetch(e);
   }
 }
 
 // Workgroups [0, n_runs): windows of rows, for up to 4 KV heads each.  The others: queries.
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kMaxWaves) void append_byte_kernel(ByteAppendParams a, int window, int n_runs,
-                                                                   int query_rows) {
+// BRIEF: with a path of their own for runs of one or two rows.
+template <typename T, int D, bool BRIEF>
+__global__ __launch_bounds__(64 * kMaxWaves, BRIEF || (sizeof(T) == 4 && D == 128) ? 4 : 6)
+void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_rows) {
   constexpr int LR = D / 16;        // lanes of a token's head
   constexpr int RP = 64 / LR;       // tokens that the lanes hold
   constexpr int SL = kByteBlock / RP;  // tokens of a lane
   __shared__ f64x2 s_cs[kByteBlock * D / 2];
   __shared__ int s_row[kMaxWaves][kByteBlock];  // the run's row of each token of the block, or -1
+  __shared__ uint64_t s_bad[2][kMaxWaves][SL];  // lanes whose token is not finite there
   const RowParams &p = a.rows;
   if ((int)blockIdx.x >= n_runs) {
     const int row0 = ((int)blockIdx.x - n_runs) * query_rows;
@@ -192,9 +198,10 @@ __global__ __launch_bounds__(64 * kMaxWaves) void append_byte_kernel(ByteAppendP
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int waves = blockDim.x >> 6, head_groups = (p.n_kv_heads + waves - 1) / waves;
+  const int heads = blockDim.x >> 7, head_groups = (p.n_kv_heads + heads - 1) / heads;
   const int row0 = (int)blockIdx.x / head_groups * window;
-  const int h = (int)blockIdx.x % head_groups * waves + wave;
+  const int h = (int)blockIdx.x % head_groups * heads + (wave >> 1);
+  const bool keys = !(wave & 1);
   const int r = p.mx.rows_per_seq, half = p.rope.half;
   const bool adjacent = p.rope.adjacent != 0;
 
@@ -203,8 +210,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void append_byte_kernel(ByteAppendP
   const int at = i < p.n ? p.pos[i] : -1;
   const int back = row0 - 64 + lane;
   const int back_at = back >= 0 ? p.pos[back] : -1;
+  const int seq = (int)((uint32_t)min(i, p.n - 1) / (uint32_t)r);
+  const int held_at = a.n_held ? a.n_held[seq] : 0;
   const bool live = (uint32_t)at < (uint32_t)p.mx.n_ctx;
-  const int block = at >> 4, seq = (int)((uint32_t)min(i, p.n - 1) / (uint32_t)r);
+  const int block = at >> 4;
+  // (what a run needs to know is asked for a row a lane, before the runs are known)
+  const int page_at = mx_page(p.mx, seq, live ? at : 0);
   static_assert(kByteBlock == 16, "blocks of positions");
   const uint64_t lives = __ballot(live), in_window = (1ull << window) - 1;  // (window < 64)
   const uint64_t before = lives & ((1ull << lane) - 1);
@@ -235,68 +246,207 @@ __global__ __launch_bounds__(64 * kMaxWaves) void append_byte_kernel(ByteAppendP
   const int l = lane % LR;
   const LaneDims d = lane_dims<D>(l, half, adjacent);
   const int gap = half / kVec % 4 && !adjacent ? 4 : 0;
-  while (leaders | outs) {
-    const int first = __builtin_ctzll(leaders | outs);
-    const bool out = outs >> first & 1;
-    leaders &= ~(1ull << first);
-    outs &= ~(1ull << first);
-    const int run_block = __builtin_amdgcn_readlane(block, first), run_seq = __builtin_amdgcn_readlane(seq, first);
-    int *rows = s_row[wave];
-
-    // The run's rows.
-    const bool member = out ? lane == first : live && lane >= first && block == run_block && seq == run_seq;
+  // A run: its rows (the row of each token of its block, or -1), the tokens that they are, and
+  // what the block keeps.
+  int *rows = s_row[wave];
+  struct Run {
+    bool out;
+    int seq, token0, page;
+    uint32_t written, kept;
+  };
+  auto run_of = [&](int first) __attribute__((always_inline)) {
+    Run x;
+    x.out = outs >> first & 1;
+    x.seq = __builtin_amdgcn_readlane(seq, first);
+    const int run_block = __builtin_amdgcn_readlane(block, first);
+    const bool member = x.out ? lane == first : live && lane >= first && block == run_block && seq == x.seq;
     wave_lds_fence();
     if (lane < kByteBlock) rows[lane] = -1;
     wave_lds_fence();
-    if (member) rows[out ? 0 : at & (kByteBlock - 1)] = i;
+    if (member) atomicMax(&rows[x.out ? 0 : at & (kByteBlock - 1)], i);
     wave_lds_fence();
-    if (!out && !__ballot(live && lane > first && !member) && rows[kByteBlock - 1] < 0) {
+    if (!x.out && !__ballot(live && lane > first && !member) && rows[kByteBlock - 1] < 0) {
       // no other row among these 64: the run may go on behind them
-      const int end = min((int64_t)(run_seq + 1) * r, (int64_t)p.n);
+      const int end = min((int64_t)(x.seq + 1) * r, (int64_t)p.n);
       for (int base = row0 + 64; base < end; base += 256) {
-        int x[4];
+        int y[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = base + 64 * k + lane < end ? p.pos[base + 64 * k + lane] : -1;
+        for (int k = 0; k < 4; ++k) y[k] = base + 64 * k + lane < end ? p.pos[base + 64 * k + lane] : -1;
         bool other = false;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          if ((uint32_t)x[k] >= (uint32_t)p.mx.n_ctx) continue;
-          if (x[k] >> 4 == run_block) rows[x[k] & (kByteBlock - 1)] = base + 64 * k + lane;
+          if ((uint32_t)y[k] >= (uint32_t)p.mx.n_ctx) continue;
+          if (y[k] >> 4 == run_block) atomicMax(&rows[y[k] & (kByteBlock - 1)], base + 64 * k + lane);
           else other = true;
         }
         if (__ballot(other)) break;
       }
       wave_lds_fence();
     }
-    const uint32_t written = (uint32_t)__ballot(rows[lane & (kByteBlock - 1)] >= 0) & 0xffffu;
+    x.written = (uint32_t)__ballot(rows[lane & (kByteBlock - 1)] >= 0) & 0xffffu;
+    x.token0 = x.out ? 0 : run_block * kByteBlock;
+    x.page = __builtin_amdgcn_readlane(page_at, first);
+    const int held = x.out          ? 0
+                     : a.n_held ? min(max(__builtin_amdgcn_readlane(held_at, first), 0), p.mx.n_ctx)
+                                    : x.token0 + 31 - __builtin_clz(x.written);
+    x.kept = ~x.written & ((1u << min(max(held - x.token0, 0), kByteBlock)) - 1);
+    return x;
+  };
+  // Codes and scale byte of a run's block for one head.
+  struct Place {
+    uint8_t *codes, *scale;
+  };
+  auto place = [&](const Run &x, int head, bool k) __attribute__((always_inline)) {
+    const int64_t slot = ((int64_t)head << p.mx.shift) + (x.token0 & ((1 << p.mx.shift) - 1));
+    return Place{(k ? p.mx.k : p.mx.v) + x.page * p.mx.code_stride + slot * D,
+                 (k ? p.mx.k_scale : p.mx.v_scale) + x.page * p.mx.scale_stride + slot / kByteBlock};
+  };
+  auto encode = [&](const Raw<T> &raw, uint32_t m, float s, bool bad, bool k) __attribute__((always_inline)) {
+    float x[kVec];
+    expand(raw, x);
+    if (m > 0x7f600000u)  // above 448 * 2^(246 - 127): the largest code
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) x[j] = fminf(fmaxf(x[j], -0x1.cp127f), 0x1.cp127f);
+    const uint2 c = encode8(x, s);
+    return !bad ? c : k ? make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu) : make_uint2(0, 0);
+  };
+  auto give_back = [&](T *held, int row, int head, const uint2 (&c)[2], float s) __attribute__((always_inline)) {
+    T *dst = held + ((int64_t)row * p.n_kv_heads + head) * D;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      float z[kVec];
+      decode8(c[y], s, z);
+      store(dst + d.at[y], z, gap);
+    }
+  };
+  auto again = [&](uint2 c, float step) __attribute__((always_inline)) {
+    float z[kVec];
+    decode8(c, 1.f, z);
+    return encode8(z, step);
+  };
+
+  // Runs of one or two rows (and rows that are left out): a wave each, side by side.
+  uint64_t brief = 0;
+  if constexpr (BRIEF) {
+    const uint64_t all_leaders = __ballot(live && !continues), later = lane < 63 ? all_leaders >> (lane + 1) : 0;
+    const int next = later ? lane + 1 + __builtin_ctzll(later) : 64;
+    const uint64_t own = lives >> lane & (next < 64 ? (1ull << (next - lane)) - 1 : ~0ull);
+    brief = (__ballot(__builtin_popcountll(own) <= 2 && (next < 64 || row0 + 64 >= p.n)) & leaders) | outs;
+  }
+  if (BRIEF && (int)blockIdx.x % head_groups == 0) {  // (one workgroup for all heads here)
+    constexpr int kUnits = 64 / LR;  // heads' keys or values side by side
+    const int n_units = 2 * p.n_kv_heads;
+    f64x2 *cs = s_cs + 2 * wave * half;
+    uint64_t todo = brief;
+    for (int skip = wave; skip > 0; --skip) todo &= todo - 1;
+    while (todo) {
+      const Run x = run_of(__builtin_ctzll(todo));
+      for (int skip = 2 * heads; skip > 0; --skip) todo &= todo - 1;
+      int token[2], row[2];  // (one: the same twice)
+      token[0] = __builtin_ctz(x.written);
+      token[1] = 31 - __builtin_clz(x.written);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) row[y] = __builtin_amdgcn_readfirstlane(rows[token[y]]);
+      for (int u0 = 0; u0 < n_units; u0 += kUnits) {
+        const int u = min(u0 + lane / LR, n_units - 1), head = u >> 1;
+        const bool k = !(u & 1), valid = u0 + lane / LR < n_units;
+        const T *src = static_cast<const T *>(k ? p.k_new : p.v_new) + head * D;
+        const int64_t stride = k ? p.k_new_stride : p.v_new_stride;
+        Raw<T> raw[2][2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) raw[y][z] = load_raw<T>(src + row[y] * stride + d.at[z]);
+        const Place at_place = place(x, head, k);
+        const int was = min(max((int)*at_place.scale, kByteScaleMin), kByteScaleMax);
+        if (half && !u0) {
+          for (int e = lane; e < 2 * half; e += 64) {
+            const int y = e >= half;
+            cs[e] = angle(p.rope, y ? row[1] : row[0], y ? e - half : e);
+          }
+          wave_lds_fence();
+        }
+        bool bad[2];
+        uint32_t m = 0;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          if (half && k) {
+            float z[2][kVec];
+            expand(raw[y][0], z[0]);
+            expand(raw[y][1], z[1]);
+            turn<D>(z, d, half, adjacent, cs + y * half);
+            as_held(z[0], raw[y][0]);
+            as_held(z[1], raw[y][1]);
+          }
+          const uint32_t largest = max(largest_bits(raw[y][0]), largest_bits(raw[y][1]));
+          const uint64_t any = __ballot(largest >= 0x7f800000u);  // of a head's keys and values
+          bad[y] = any >> (lane & ~(2 * LR - 1)) & ((1ull << (2 * LR)) - 1);
+          m = max(m, bad[y] ? 0 : largest);
+        }
+        m = max(m, dpp_mov<kDppXor1>(0u, m));
+        m = max(m, dpp_mov<kDppXor2>(0u, m));
+        if (LR == 8) m = max(m, dpp_mov<kDppHalfMirror>(0u, m));
+        if (!valid) continue;
+        int now = needed_scale(m);
+        if (x.kept) now = max(now, was);
+        const float s = two_to(now - 127);
+        T *held_out = static_cast<T *>(k ? p.k_out : p.v_out);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          if (y && token[1] == token[0]) continue;
+          const uint2 c[2] = {encode(raw[y][0], m, s, bad[y], k), encode(raw[y][1], m, s, bad[y], k)};
+          if (held_out) give_back(held_out, row[y], head, c, s);
+          if (x.out) continue;
+#pragma unroll
+          for (int z = 0; z < 2; ++z) *reinterpret_cast<uint2 *>(at_place.codes + token[y] * D + d.at[z]) = c[z];
+        }
+        if (x.out) continue;
+        if (x.kept && now > was) {
+          // four of the kept tokens on their way at a time
+          const float step = two_to(min(now - was, 64));
+          for (int t0 = 0; t0 < kByteBlock; t0 += 4) {
+            uint2 c[4][2];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int z = 0; z < 2; ++z)
+                c[t][z] = *reinterpret_cast<const uint2 *>(at_place.codes + (t0 + t) * D + d.at[z]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (x.kept >> (t0 + t) & 1)
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                  *reinterpret_cast<uint2 *>(at_place.codes + (t0 + t) * D + d.at[z]) = again(c[t][z], step);
+          }
+        }
+        if (l == 0) *at_place.scale = (uint8_t)now;
+      }
+    }
+  }
+  leaders &= ~brief;
+  outs &= ~brief;
+
+  for (int turn_of = 0; leaders | outs; turn_of ^= 1) {
+    const int first = __builtin_ctzll(leaders | outs);
+    const Run run = run_of(first);
+    leaders &= ~(1ull << first);
+    outs &= ~(1ull << first);
 
     // The lane's tokens on their way, and where the block lies.
     int row[SL];
-    Raw<T> kr[SL][2], vr[SL][2];
+    Raw<T> raw[SL][2];
+    const T *src = static_cast<const T *>(keys ? p.k_new : p.v_new) + h * D;
+    const int64_t stride = keys ? p.k_new_stride : p.v_new_stride;
 #pragma unroll
     for (int t = 0; t < SL; ++t) {
       row[t] = h < p.n_kv_heads ? rows[lane / LR + RP * t] : -1;
       if (row[t] >= 0) {
-        const T *k = static_cast<const T *>(p.k_new) + row[t] * p.k_new_stride + h * D;
-        const T *v = static_cast<const T *>(p.v_new) + row[t] * p.v_new_stride + h * D;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          kr[t][x] = load_raw<T>(k + d.at[x]);
-          vr[t][x] = load_raw<T>(v + d.at[x]);
-        }
+        for (int x = 0; x < 2; ++x) raw[t][x] = load_raw<T>(src + row[t] * stride + d.at[x]);
       }
     }
-    const int token0 = out ? 0 : run_block * kByteBlock;
-    const int64_t page = mx_page(p.mx, run_seq, token0);
-    const int64_t slot = ((int64_t)min(h, p.n_kv_heads - 1) << p.mx.shift) + (token0 & ((1 << p.mx.shift) - 1));
-    const int64_t codes = page * p.mx.code_stride + slot * D;
-    const int64_t scale = page * p.mx.scale_stride + slot / kByteBlock;
-    // tokens that the block keeps
-    const int held = out          ? 0
-                     : a.n_held ? min(max(a.n_held[run_seq], 0), p.mx.n_ctx)
-                                  : token0 + 31 - __builtin_clz(written);
-    const uint32_t kept = ~written & ((1u << min(max(held - token0, 0), kByteBlock)) - 1);
-    const int k_was = p.mx.k_scale[scale], v_was = p.mx.v_scale[scale];
+    const Place at_place = place(run, min(h, p.n_kv_heads - 1), keys);
+    const int was = min(max((int)*at_place.scale, kByteScaleMin), kByteScaleMax);
 
     // The run's angles.
     if (half) {
@@ -308,83 +458,64 @@ __global__ __launch_bounds__(64 * kMaxWaves) void append_byte_kernel(ByteAppendP
       __syncthreads();
     }
 
-    bool bad[SL];  // a token with an infinity or a NaN among its keys or values: NaN keys, zero values
-    uint32_t km = 0, vm = 0;
+    uint32_t largest[SL];
 #pragma unroll
     for (int t = 0; t < SL; ++t) {
-      uint32_t m = 0, n = 0;
+      largest[t] = 0;
       if (row[t] >= 0) {
-        if (half) {
+        if (half && keys) {
           float x[2][kVec];
-          expand(kr[t][0], x[0]);
-          expand(kr[t][1], x[1]);
+          expand(raw[t][0], x[0]);
+          expand(raw[t][1], x[1]);
           turn<D>(x, d, half, adjacent, s_cs + (lane / LR + RP * t) * half);
-          as_held(x[0], kr[t][0]);
-          as_held(x[1], kr[t][1]);
+          as_held(x[0], raw[t][0]);
+          as_held(x[1], raw[t][1]);
         }
-        m = max(largest_bits(kr[t][0]), largest_bits(kr[t][1]));
-        n = max(largest_bits(vr[t][0]), largest_bits(vr[t][1]));
+        largest[t] = max(largest_bits(raw[t][0]), largest_bits(raw[t][1]));
       }
-      const uint64_t any = __ballot(max(m, n) >= 0x7f800000u);
-      bad[t] = any >> (lane - l) & ((1ull << LR) - 1);
-      km = max(km, bad[t] ? 0 : m);
-      vm = max(vm, bad[t] ? 0 : n);
+      const uint64_t any = __ballot(largest[t] >= 0x7f800000u);
+      if (lane == 0) s_bad[turn_of][wave][t] = any;
     }
-    auto most = [](uint32_t x, uint32_t y) { return max(x, y); };
-    km = wave_reduce(km, 0u, most);
-    vm = wave_reduce(vm, 0u, most);
+    __syncthreads();
+    // A token with an infinity or a NaN among its keys or values has NaN keys and zero values,
+    // and no say in the scale.
+    bool bad[SL];
+    uint32_t m = 0;
+#pragma unroll
+    for (int t = 0; t < SL; ++t) {
+      const uint64_t any = s_bad[turn_of][wave][t] | s_bad[turn_of][wave ^ 1][t];
+      bad[t] = any >> (lane - l) & ((1ull << LR) - 1);
+      m = max(m, bad[t] ? 0 : largest[t]);
+    }
+    m = wave_reduce(m, 0u, [](uint32_t x, uint32_t y) { return max(x, y); });
     if (h >= p.n_kv_heads) continue;
 
-    auto finish = [&](const Raw<T> (&raw)[SL][2], uint32_t m, int was, uint8_t *pool, uint8_t *scales, void *held_out,
-                      bool keys) __attribute__((always_inline)) {
-      int now = needed_scale(m);
-      was = min(max(was, kByteScaleMin), kByteScaleMax);
-      if (kept) now = max(now, was);
-      const float s = two_to(now - 127);
-      const bool rises = kept && now > was;
-      const float step = two_to(min(now - was, 64));
+    int now = needed_scale(m);
+    if (run.kept) now = max(now, was);
+    const float s = two_to(now - 127);
+    const bool rises = run.kept && now > was;
+    const float step = two_to(min(now - was, 64));
+    T *held_out = static_cast<T *>(keys ? p.k_out : p.v_out);
 #pragma unroll
-      for (int t = 0; t < SL; ++t) {
-        const int token = lane / LR + RP * t;
-        uint2 c[2];
-        if (row[t] >= 0) {
+    for (int t = 0; t < SL; ++t) {
+      const int token = lane / LR + RP * t;
+      uint2 c[2];
+      if (row[t] >= 0) {
+        c[0] = encode(raw[t][0], m, s, bad[t], keys);
+        c[1] = encode(raw[t][1], m, s, bad[t], keys);
+        if (held_out) give_back(held_out, row[t], h, c, s);
+        if (run.out) continue;
+      } else if (rises && run.kept >> token & 1) {
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float x[kVec];
-            expand(raw[t][y], x);
-            if (m > 0x7f600000u)  // above 448 * 2^(246 - 127): the largest code
-#pragma unroll
-              for (int j = 0; j < kVec; ++j) x[j] = fminf(fmaxf(x[j], -0x1.cp127f), 0x1.cp127f);
-            c[y] = encode8(x, s);
-            if (bad[t]) c[y] = keys ? make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu) : make_uint2(0, 0);
-          }
-          if (held_out) {
-            T *dst = static_cast<T *>(held_out) + ((int64_t)row[t] * p.n_kv_heads + h) * D;
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              float z[kVec];
-              decode8(c[y], s, z);
-              store(dst + d.at[y], z, gap);
-            }
-          }
-        } else if (rises && kept >> token & 1) {
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float z[kVec];
-            decode8(*reinterpret_cast<const uint2 *>(pool + codes + token * D + d.at[y]), 1.f, z);
-            c[y] = encode8(z, step);
-          }
-        } else {
-          continue;
-        }
-        if (out) continue;
-#pragma unroll
-        for (int y = 0; y < 2; ++y) *reinterpret_cast<uint2 *>(pool + codes + token * D + d.at[y]) = c[y];
+        for (int y = 0; y < 2; ++y)
+          c[y] = again(*reinterpret_cast<const uint2 *>(at_place.codes + token * D + d.at[y]), step);
+      } else {
+        continue;
       }
-      if (!out && lane == 0) scales[scale] = (uint8_t)now;
-    };
-    finish(kr, km, k_was, p.mx.k, p.mx.k_scale, p.k_out, true);
-    finish(vr, vm, v_was, p.mx.v, p.mx.v_scale, p.v_out, false);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) *reinterpret_cast<uint2 *>(at_place.codes + token * D + d.at[y]) = c[y];
+    }
+    if (!run.out && lane == 0) *at_place.scale = (uint8_t)now;
   }
 }
 
@@ -392,11 +523,14 @@ template <typename T, int D>
 void launch(const ByteAppendParams &a, hipStream_t s) {
   const RowParams &p = a.rows;
   const bool many = p.n >= kWindowFrom;
-  const int window = many ? kWindow : 1, query_rows = many ? kQueryRows : 1;
-  const int waves = std::min(p.n_kv_heads, kMaxWaves), groups = (p.n_kv_heads + waves - 1) / waves;
+  const int window = many ? kWindow : kWindowFew, query_rows = p.n >= kQueryRowsFrom ? kQueryRows : 1;
+  const int heads = std::min(p.n_kv_heads, kMaxHeads), groups = (p.n_kv_heads + heads - 1) / heads;
   const int n_runs = (p.n + window - 1) / window * groups;
   const int grid = n_runs + (p.n_q_heads ? (p.n + query_rows - 1) / query_rows : 0);
-  append_byte_kernel<T, D><<<grid, 64 * waves, 0, s>>>(a, window, n_runs, query_rows);
+  if (many)
+    append_byte_kernel<T, D, false><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, query_rows);
+  else
+    append_byte_kernel<T, D, true><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, query_rows);
 }
 
 }  // namespace

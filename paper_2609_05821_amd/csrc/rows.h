@@ -13,31 +13,37 @@ typedef double f64x2 __attribute__((ext_vector_type(2)));
 
 // (cos, sin) of a = p * f: a is reduced by the nearest multiple of pi/2 (two-part
 // constant, fused multiply-adds), then Taylor series on [-pi/4, pi/4], whose
-// first omitted terms are below 5e-17.
+// first omitted terms are below 5e-17.  SCALAR: constants in scalar registers (in a kernel with
+// a loop around, where they would be held in 30 vector registers).
+template <bool SCALAR = false>
 __device__ __forceinline__ f64x2 cos_sin(double a) {
+  auto k_ = [](double x) __attribute__((always_inline)) {
+    if constexpr (SCALAR) asm("" : "+s"(x));
+    return x;
+  };
   // (1.5 * 2^52 leaves the integer in the low bits; |a| < 2^41.01)
   const double shifted = __builtin_fma(a, 0.63661977236758134308, 6755399441055744.0);
   const double k = shifted - 6755399441055744.0;
   double r = __builtin_fma(-k, 1.57079632679489655800e+00, a);
   r = __builtin_fma(-k, 6.12323399573676603587e-17, r);
   const double z = r * r;
-  double s = -1.0 / 1307674368000.0;                        // 1/15!
-  s = __builtin_fma(s, z, 1.0 / 6227020800.0);              // 1/13!
-  s = __builtin_fma(s, z, -1.0 / 39916800.0);
-  s = __builtin_fma(s, z, 1.0 / 362880.0);
-  s = __builtin_fma(s, z, -1.0 / 5040.0);
-  s = __builtin_fma(s, z, 1.0 / 120.0);
-  s = __builtin_fma(s, z, -1.0 / 6.0);
+  double s = k_(-1.0 / 1307674368000.0);                        // 1/15!
+  s = __builtin_fma(s, z, k_(1.0 / 6227020800.0));              // 1/13!
+  s = __builtin_fma(s, z, k_(-1.0 / 39916800.0));
+  s = __builtin_fma(s, z, k_(1.0 / 362880.0));
+  s = __builtin_fma(s, z, k_(-1.0 / 5040.0));
+  s = __builtin_fma(s, z, k_(1.0 / 120.0));
+  s = __builtin_fma(s, z, k_(-1.0 / 6.0));
   s = __builtin_fma(s * z, r, r);
-  double c = 1.0 / 20922789888000.0;                        // 1/16!
-  c = __builtin_fma(c, z, -1.0 / 87178291200.0);            // 1/14!
-  c = __builtin_fma(c, z, 1.0 / 479001600.0);
-  c = __builtin_fma(c, z, -1.0 / 3628800.0);
-  c = __builtin_fma(c, z, 1.0 / 40320.0);
-  c = __builtin_fma(c, z, -1.0 / 720.0);
-  c = __builtin_fma(c, z, 1.0 / 24.0);
-  c = __builtin_fma(c, z, -0.5);
-  c = __builtin_fma(c, z, 1.0);
+  double c = k_(1.0 / 20922789888000.0);                        // 1/16!
+  c = __builtin_fma(c, z, k_(-1.0 / 87178291200.0));            // 1/14!
+  c = __builtin_fma(c, z, k_(1.0 / 479001600.0));
+  c = __builtin_fma(c, z, k_(-1.0 / 3628800.0));
+  c = __builtin_fma(c, z, k_(1.0 / 40320.0));
+  c = __builtin_fma(c, z, k_(-1.0 / 720.0));
+  c = __builtin_fma(c, z, k_(1.0 / 24.0));
+  c = __builtin_fma(c, z, k_(-0.5));
+  c = __builtin_fma(c, z, k_(1.0));
   const int q = (int)__builtin_bit_cast(uint64_t, shifted) & 3;  // k mod 4
   const double cc = q & 1 ? s : c, ss = q & 1 ? c : s;
   return f64x2{q == 1 || q == 2 ? -cc : cc, q >= 2 ? -ss : ss};

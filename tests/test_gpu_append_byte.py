@@ -162,7 +162,7 @@ def test_rows_left_out(gaps):
     append(c, pos, k, v * 9, held=False, n_held=torch.tensor([30, 400], dtype=torch.int32))
 
 
-@pytest.mark.parametrize("n", [4095, 4096, 4500, 5000])
+@pytest.mark.parametrize("n", [511, 512, 4500, 8191, 8192, 10000])
 @pytest.mark.parametrize("hkv", [1, 5])
 def test_many_rows(n, hkv):
     """Either side of the number of rows from which workgroups take 16 each; first positions
@@ -184,15 +184,24 @@ def test_many_rows(n, hkv):
     assert torch.equal(q_out, want)
 
 
-def test_scattered_rows_in_windows():
-    """Windows of 16 rows that begin many runs, and runs that begin in one window and end in
-    the next."""
-    ctx = 9000
+@pytest.mark.parametrize("n,ctx,hkv,d", [(900, 9000, 2, 64), (800, 1100, 6, 128), (8300, 30000, 1, 64)])
+def test_scattered_rows_in_windows(n, ctx, hkv, d):
+    """Windows that begin many runs, short and long ones, runs that begin in one window and end
+    in the next; more heads than a workgroup takes."""
     g = torch.Generator().manual_seed(0)
-    c = Cache(1, ctx, 2, 2, 64, page=1024, seed=1)
-    pos = torch.randperm(ctx, generator=g)[:4300].sort().values.to(torch.int32)
-    _, k, v = new_rows(4300, 2, 2, 64, "bf16", 3)
-    append(c, pos, k, v * 5, n_held=torch.tensor([ctx - 100], dtype=torch.int32))
+    c = Cache(1, ctx, hkv, hkv, d, page=1024, seed=1)
+    pos = torch.randperm(ctx, generator=g)[:n].sort().values.to(torch.int32)
+    _, k, v = new_rows(n, hkv, hkv, d, "bf16", 3)
+    rope, rp = rope_of(d // 4, 1, 0), torch.randint(0, 9000, (1, n), generator=g, dtype=torch.int32).to(DEV)
+    append(c, pos, k, v * 5, n_held=torch.tensor([ctx - 100], dtype=torch.int32), rope=rope, rp=rp)
+
+
+def test_the_last_of_rows_with_one_position():
+    """Rows that share a position, in a short run, a long one and across windows."""
+    c = Cache(1, 200, 2, 2, 64, seed=12)
+    pos = torch.tensor([3, 3, 20, 21, 21, 22, 22, 22, 40, 41, 42, 43, 44, 45, 46, 46, 47, 48, 48], dtype=torch.int32)
+    _, k, v = new_rows(len(pos), 2, 2, 64, "bf16", 5)
+    append(c, pos, k, v, held=False, n_held=torch.tensor([200], dtype=torch.int32))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
