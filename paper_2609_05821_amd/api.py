@@ -605,9 +605,11 @@ def _call(fn, tensors, stream, *args) -> None:
         _check(status)
 
 
-def _heads(t: torch.Tensor, what: str) -> int:
-    """Row stride of [n, H, d] with dense heads (any row stride)."""
-    shape, stride = t.shape, t.stride()
+def _heads(t: torch.Tensor, what: str, shape=None) -> int:
+    """Row stride of [n, H, d] with dense heads (any row stride); shape: t's, where the caller has it."""
+    if shape is None:
+        shape = t.shape
+    stride = t.stride()
     if len(shape) != 3 or stride[2] != 1 or (shape[1] != 1 and stride[1] != shape[2]):
         raise ConduitError(ERR_INVALID_ARG, f"{what} must be [n, H, d] with dense heads")
     return stride[0] if shape[0] > 1 else shape[1] * shape[2]
@@ -627,10 +629,11 @@ def _rope_args(rope: Optional[Rope], rope_pos: Optional[torch.Tensor], n: int):
         return None, None, 0
     if rope_pos.dim() == 1:
         rope_pos = rope_pos[None]
-    if rope_pos.dtype != torch.int32 or rope_pos.shape != (rope.n_axes, n) or (n > 1 and rope_pos.stride(1) != 1) or \
-            (rope.n_axes > 1 and rope_pos.stride(0) < n):
-        raise ConduitError(ERR_INVALID_ARG, f"rope_pos must be int32 [{rope.n_axes}, {n}], rows dense and apart")
-    return ctypes.byref(rope.desc), rope_pos.data_ptr(), max(rope_pos.stride(0), n)
+    axes, stride = rope.n_axes, rope_pos.stride()
+    if rope_pos.dtype is not torch.int32 or rope_pos.shape != (axes, n) or (n > 1 and stride[1] != 1) or \
+            (axes > 1 and stride[0] < n):
+        raise ConduitError(ERR_INVALID_ARG, f"rope_pos must be int32 [{axes}, {n}], rows dense and apart")
+    return ctypes.byref(rope.desc), rope_pos.data_ptr(), stride[0] if stride[0] > n else n
 
 
 def conduit_rotary(x: torch.Tensor, rope: Rope, rope_pos: torch.Tensor, out: torch.Tensor, inverse: bool = False,
@@ -648,20 +651,24 @@ def conduit_rotary(x: torch.Tensor, rope: Rope, rope_pos: torch.Tensor, out: tor
 
 
 def _new_rows(k_new, v_new, q, q_out, n_q_heads: int, n_kv_heads: int, d: int) -> Rows:
-    n = k_new.shape[0]
-    ks, vs = _heads(k_new, "k_new"), _heads(v_new, "v_new")
-    if k_new.shape != (n, n_kv_heads, d) or v_new.shape != k_new.shape:
+    shape = k_new.shape
+    n = shape[0]
+    ks, vs = _heads(k_new, "k_new", shape), _heads(v_new, "v_new")
+    if shape != (n, n_kv_heads, d) or v_new.shape != shape:
         raise ConduitError(ERR_INVALID_ARG, f"k_new and v_new must be [n, {n_kv_heads}, {d}]")
     if (q is None) != (q_out is None):
         raise ConduitError(ERR_INVALID_ARG, "q and q_out go together")
-    if any(t is not None and t.dtype != k_new.dtype for t in (v_new, q, q_out)):
+    dtype = k_new.dtype
+    if v_new.dtype is not dtype or (q is not None and (q.dtype is not dtype or q_out.dtype is not dtype)):
         raise ConduitError(ERR_INVALID_ARG, "k_new, v_new, q and q_out must have one dtype")
-    qs = qos = 0
-    if q is not None:
-        qs, qos = _heads(q, "q"), _heads(q_out, "q_out")
-        if q.shape != (n, n_q_heads, d) or q_out.shape != q.shape:
-            raise ConduitError(ERR_INVALID_ARG, f"q and q_out must be [n, {n_q_heads}, {d}]")
-    return Rows(n, _dtype_code(k_new), _ptr(k_new), _ptr(v_new), ks, vs, _ptr(q), _ptr(q_out), qs, qos)
+    if q is None:
+        return Rows(n, _dtype_code(k_new), k_new.data_ptr(), v_new.data_ptr(), ks, vs, None, None, 0, 0)
+    qshape = q.shape
+    qs, qos = _heads(q, "q", qshape), _heads(q_out, "q_out")
+    if qshape != (n, n_q_heads, d) or q_out.shape != qshape:
+        raise ConduitError(ERR_INVALID_ARG, f"q and q_out must be [n, {n_q_heads}, {d}]")
+    return Rows(n, _dtype_code(k_new), k_new.data_ptr(), v_new.data_ptr(), ks, vs, q.data_ptr(), q_out.data_ptr(), qs,
+                qos)
 
 
 def conduit_append_kv(kv: KV, pos: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
@@ -755,9 +762,11 @@ def conduit_append_byte(cache: KVByte, pos: torch.Tensor, k_new: torch.Tensor, v
     if n_held is not None:
         _row_ids(n_held, cache.n_seqs, "n_held")
     desc, rp, ps = _rope_args(rope, rope_pos, rows.n)
+    # (the cache's tensors are on one device since it was described: the first speaks for all)
     _call(lib().conduit_append_byte,
-          (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), n_held, rope_pos, *_held(cache)), stream,
-          ctypes.byref(cache), ctypes.byref(rows), _ptr(pos), _ptr(n_held), desc, rp, ps, _ptr(k_out), _ptr(v_out))
+          (k_new, v_new, q, q_out, k_out, v_out, _row_ids(pos, rows.n, "pos"), n_held, rope_pos, *_held(cache)[:1]),
+          stream, ctypes.byref(cache), ctypes.byref(rows), pos.data_ptr(), _ptr(n_held), desc, rp, ps, _ptr(k_out),
+          _ptr(v_out))
 
 
 def conduit_load_byte(cache: KVByte, src_pos: torch.Tensor, kv: KV, dst_pos: torch.Tensor, rope: Optional[Rope] = None,
@@ -767,7 +776,7 @@ def conduit_load_byte(cache: KVByte, src_pos: torch.Tensor, kv: KV, dst_pos: tor
     n = src_pos.numel()
     desc, rp, ps = _rope_args(rope, rope_pos, n)
     ids = _row_ids(src_pos, n, "src_pos"), _row_ids(dst_pos, n, "dst_pos")
-    _call(lib().conduit_load_byte, (*ids, rope_pos, *_held(cache), *_held(kv)), stream, ctypes.byref(cache),
+    _call(lib().conduit_load_byte, (*ids, rope_pos, *_held(cache)[:1], *_held(kv)), stream, ctypes.byref(cache),
           _ptr(src_pos), n, ctypes.byref(kv), _ptr(dst_pos), desc, rp, ps)
 
 
