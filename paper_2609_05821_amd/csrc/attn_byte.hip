@@ -336,7 +336,10 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr int kManyWaves = 8;
 constexpr int kManyThreads = 64 * kManyWaves;
 constexpr int kBytePairs = 32 * kManyWaves;          // pairs of a block
-constexpr int kManyPad = 3;                          // what beginning a block costs, in tiles
+// What beginning a block costs, in tiles: its first tiles and queries, and the rows of the part
+// that it leaves for the merge.  (1,638 rows over 17,024 keys: 1 tile 273 us, 3 242, 6 232, 8 234,
+// 12 237, 16 240; 4 sequences of 333 rows over 4,100 states: 3 95, 6 93, 12 100.)
+constexpr int kManyPad = 6;
 constexpr int kRing = 4;                             // tiles in LDS
 constexpr float kHead = 11.f, kManySlack = 4.f;      // weights stay below 2^(kHead + kManySlack)
 constexpr float kFar = 89.f;
@@ -366,7 +369,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
   const int hkv = p.mx.n_kv_heads, r = p.mx.rows_per_seq, G = p.group;
   const int n_sb = p.n_seqs * p.blocks_per_seq;
   Part part{0, 1, 0, 0, 0, 0};
-  if (p.n_workers && !plan_part<kManyWaves, 32, kManyPad>(p, kPairs, kTileKeys, s_sum, s_prefix, part)) return;
+  if (p.n_workers && !plan_part<kManyWaves, 8, kManyPad, true>(p, kPairs, kTileKeys, s_sum, s_prefix, part)) return;
   const int part0 = part.t;
   const MxCache &c = p.mx;
   const int v_lane = v_operand_lane_offset_il<VP>(lane);
@@ -726,8 +729,9 @@ template <int D>
 void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStream_t s) {
   const int n_sb = p.n_seqs * p.blocks_per_seq;
   const int grid = p.n_workers ? p.n_workers : n_sb * p.mx.n_kv_heads;
-  const size_t lds = p.n_workers && n_sb > kLaneBlocks ? (size_t)(n_sb + 1) * 4 : 0;
-  if (sh.pairs == kBytePairs)
+  const bool many = sh.pairs == kBytePairs;
+  const size_t lds = p.n_workers && (many || n_sb > kLaneBlocks) ? (size_t)(n_sb + 1) * 4 : 0;
+  if (many)
     attn_byte_many_kernel<D><<<grid, kManyThreads, lds, s>>>(p);
   else if (p.n_workers || grid > 256)
     launch_few<D, 4>(p, sh.pairs > 16, bf16, grid, lds, s);
@@ -737,11 +741,28 @@ void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStre
 
 }  // namespace
 
+// Whether a block takes kBytePairs pairs.  Such a block reads and decodes its keys once, but takes
+// 13 us for its first tile and is at work on one CU alone; blocks of 32 pairs read the cache again
+// for every 32, and spread over the chip.  4 KV heads, blocks of 32 and of 256 pairs, in us, D = 128:
+//   sequences x keys     64 pairs     128         256         512
+//   1 x 8,192            16   20      21   24     27   31     37   34
+//   1 x 65,536           34   45      48   49     80   57    143   89
+//   8 x 4,096            26   30      38   36     61   47     93   59
+//   64 x 4,096          107  126     147  139    285  162    534  320
+//   256 x 512            60   78     103   88    198  111    404  221
+// and D = 64: 64 x 4,096 keys with 128 pairs 87 and 107, 256 pairs 155 and 119; 256 x 512: 58 and
+// 65, 110 and 76.  Short caches that leave CUs idle go to blocks of 32 (1 x 1,024 keys with 512
+// pairs 16 and 37).
+inline bool many_pairs(int64_t n_seqs, int64_t n_kv_heads, int64_t n_ctx, int head_dim, int64_t pairs, bool bf16) {
+  return bf16 && pairs > (head_dim == 128 ? 64 : 128) &&
+         n_seqs * n_kv_heads * ((pairs + 31) / 32) > ((1 << 18) - 1) / std::max<int64_t>(n_ctx, 1);
+}
+
 MxAttnShape byte_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_ctx,
                           int32_t head_dim, bool bf16) {
   MxAttnShape L{};
   const int64_t pairs = (int64_t)rows_per_seq * (n_q_heads / n_kv_heads);
-  const bool many = bf16 && pairs > 32;
+  const bool many = many_pairs(n_seqs, n_kv_heads, n_ctx, head_dim, pairs, bf16);
   L.pairs = many ? kBytePairs : few_pairs(head_dim, pairs, bf16);
   L.blocks_per_seq = (int32_t)((pairs + L.pairs - 1) / L.pairs);
   const int64_t n_sb = (int64_t)n_seqs * L.blocks_per_seq, blocks = n_sb * n_kv_heads;

@@ -88,6 +88,30 @@ __device__ __forceinline__ int block_steps(const MxAttnParams &p, int sb, int pa
   return (keys_seen(top, p.mx.n_ctx) + step - 1) / step;
 }
 
+// The most keys that a row of each sequence block sees, found by the whole workgroup: a row a
+// thread, kept per block in LDS.  (A thread that reads the up to 256 rows of a block of its own
+// waits for them in turn: 12 us of one sequence's 8,192 rows in blocks of 256.)
+template <int W>
+__device__ __forceinline__ void block_tops(const MxAttnParams &p, int pairs, int *s_top) {
+  constexpr int kThreads = 64 * W, kBatch = 8;
+  const int tid = threadIdx.x, n_sb = p.n_seqs * p.blocks_per_seq, r = p.mx.rows_per_seq, rows = p.n_seqs * r;
+  for (int i = tid; i < n_sb; i += kThreads) s_top[i] = 0;
+  __syncthreads();
+  for (int row0 = tid; row0 < rows; row0 += kBatch * kThreads) {
+    int x[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) x[j] = p.pos[min(row0 + j * kThreads, rows - 1)];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int row = row0 + j * kThreads;
+      if (row >= rows) break;
+      const int s = row / r, i = (row - s * r) * p.group, seen = keys_seen(x[j], p.mx.n_ctx);
+      for (int b = i / pairs; b <= (i + p.group - 1) / pairs; ++b) atomicMax(s_top + s * p.blocks_per_seq + b, seen);
+    }
+  }
+  __syncthreads();
+}
+
 // Workgroups that share `total` steps: no fewer than kMinSteps each.
 constexpr int kMinSteps = 2;
 __device__ __forceinline__ int workers(int n_workers, int total) { return min(n_workers, max(1, total / kMinSteps)); }
@@ -115,15 +139,22 @@ struct Part {
 // before its own, for what beginning it costs a workgroup (merge: the same).  With blocks of
 // many pairs, whose first products wait for queries, pages and a tile in LDS, a workgroup
 // that had ten short blocks ended long after one that had half of a long one.
-template <int W = kWaves, int BATCH = 8, int PAD = 0>
+//
+// ROWS: positions read by the whole workgroup (block_tops; s_prefix holds kLaneBlocks entries at least).
+template <int W = kWaves, int BATCH = 8, int PAD = 0, bool ROWS = false>
 __device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int step, int *s_sum, int *s_prefix,
                                           Part &part) {
   constexpr int kWaves = W, kThreads = 64 * W;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n_sb = p.n_seqs * p.blocks_per_seq, hkv = p.mx.n_kv_heads, w = blockIdx.x;
   int total = 0;
+  if constexpr (ROWS) block_tops<W>(p, pairs, s_prefix);
+  auto steps_of = [&](int sb) __attribute__((always_inline)) {
+    if constexpr (ROWS) return (s_prefix[sb] + step - 1) / step;
+    else return block_steps<BATCH>(p, sb, pairs, step);
+  };
   if (n_sb <= kLaneBlocks) {
-    part.steps = lane < n_sb ? block_steps<BATCH>(p, lane, pairs, step) : 0;
+    part.steps = lane < n_sb ? steps_of(lane) : 0;
     int own = part.steps * hkv;
     int steps = 0;  // of the call, without PAD
     if (PAD) steps = __builtin_amdgcn_readlane((int)wave_inclusive_sum((uint32_t)own), 63);
@@ -157,7 +188,7 @@ __device__ __forceinline__ bool plan_part(const MxAttnParams &p, int pairs, int 
   } else {
     for (int b0 = 0; b0 < n_sb; b0 += kThreads) {
       const int sb = b0 + tid;
-      int own = sb < n_sb ? block_steps<BATCH>(p, sb, pairs, step) * hkv : 0;
+      int own = sb < n_sb ? steps_of(sb) * hkv : 0;
       if (PAD && own) own += PAD * hkv;
       const int incl = (int)wave_inclusive_sum((uint32_t)own);
       __syncthreads();
@@ -247,6 +278,29 @@ __device__ __forceinline__ int page_number(const MxCache &c, const SeqPages &s, 
   return min(max(page, 0), c.n_pages - 1);
 }
 
+// The workgroups w0 .. w1 that worked on a KV head of a block (none: w1 < w0), and where the first's part lies.
+struct MergeParts {
+  int w0, w1, first;
+};
+__device__ __forceinline__ MergeParts merge_parts(const MxAttnParams &p, int sb, int h, int pad) {
+  const int hkv = p.mx.n_kv_heads;
+  const int base = p.prefix[sb], next = p.prefix[sb + 1], total = p.prefix[p.n_seqs * p.blocks_per_seq];
+  const int cut = *p.cut;
+  const int n = workers(p.n_workers, total), steps = (next - base) / hkv;  // (with `pad`)
+  if (steps <= 0) return {0, -1, 0};
+  if (cut) {
+    const int parts = (steps - pad + cut - 1) / cut, w0 = p.parts[sb] + h * parts;
+    return {w0, w0 + parts - 1, 2 * w0};
+  }
+  // The workgroup that holds step x is the last whose part begins at or
+  // before it (doubles: exact below 2^53, quotients far from rounding up).
+  const int t0 = base + h * steps, t1 = t0 + steps;
+  int w0 = (int)(((double)(t0 + 1) * n - 1) / total), w1 = (int)(((double)t1 * n - 1) / total);
+  int first = 2 * w0 + (part_begin(w0, total, n) >= t0 ? 0 : 1);
+  while (pad && part_begin(w0 + 1, total, n) - t0 <= pad) first = 2 * ++w0;  // (has no step of its own)
+  return {w0, w1, first};
+}
+
 // Merge of the blocks that more than one workgroup worked on, and the outputs
 // of blocks without keys.  A workgroup takes PW pairs of a block, a group of D / 4
 // lanes each; with PW = 1 all groups share the parts of one pair.
@@ -268,55 +322,39 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(MxAttnParams p, int pai
   const int j = chunk * PW + grp % PW, pair = rb * pairs + j;
   const bool out = pair < p.mx.rows_per_seq * p.group;
   if (rb * pairs + chunk * PW >= p.mx.rows_per_seq * p.group) return;
-  const int base = p.prefix[sb], next = p.prefix[sb + 1], total = p.prefix[p.n_seqs * p.blocks_per_seq];
-  const int cut = *p.cut;
-  const int n = workers(p.n_workers, total), steps = (next - base) / hkv;  // (with `pad`)
+  const auto [w0, w1, first] = merge_parts(p, sb, h, pad);
+  if (w0 == w1) return;  // written by that workgroup
   float M = kMInit, L = 0.f;
   f32x4 o{};
-  if (steps > 0) {
-    // The workgroup that holds step x is the last whose part begins at or
-    // before it (doubles: exact below 2^53, quotients far from rounding up).
-    const int t0 = base + h * steps, t1 = t0 + steps;
-    int w0 = (int)(((double)(t0 + 1) * n - 1) / total), w1 = (int)(((double)t1 * n - 1) / total);
-    int first = 2 * w0 + (part_begin(w0, total, n) >= t0 ? 0 : 1);
-    while (pad && !cut && part_begin(w0 + 1, total, n) - t0 <= pad) first = 2 * ++w0;  // (has no step of its own)
-    if (cut) {
-      const int parts = (steps - pad + cut - 1) / cut;
-      w0 = p.parts[sb] + h * parts;
-      w1 = w0 + parts - 1;
-      first = 2 * w0;
-    }
-    if (w0 == w1) return;  // written by that workgroup
-    if (out)
-      for (int w = w0 + share; w <= w1; w += kBatch * kShare) {
-        float2 ml[kBatch];
-        f32x4 x[kBatch];
+  if (out)
+    for (int w = w0 + share; w <= w1; w += kBatch * kShare) {
+      float2 ml[kBatch];
+      f32x4 x[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const int wi = w + i * kShare;
-          ml[i] = make_float2(kMInit, 0.f);
-          x[i] = f32x4{};
-          if (wi <= w1) {
-            const int64_t slot = wi == w0 ? first : 2 * wi;
-            ml[i] = p.part_ml[slot * pairs + j];
-            x[i] = *reinterpret_cast<const f32x4 *>(p.part_o + (slot * pairs + j) * D + e);
-          }
-        }
-        float mn = M;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) mn = fmaxf(mn, ml[i].x);
-        const float a = fast_exp2(M - mn);
-        M = mn;
-        L *= a;
-        o *= a;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const float b = fast_exp2(ml[i].x - mn);
-          L += ml[i].y * b;
-          o += x[i] * b;
+      for (int i = 0; i < kBatch; ++i) {
+        const int wi = w + i * kShare;
+        ml[i] = make_float2(kMInit, 0.f);
+        x[i] = f32x4{};
+        if (wi <= w1) {
+          const int64_t slot = wi == w0 ? first : 2 * wi;
+          ml[i] = p.part_ml[slot * pairs + j];
+          x[i] = *reinterpret_cast<const f32x4 *>(p.part_o + (slot * pairs + j) * D + e);
         }
       }
-  }
+      float mn = M;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) mn = fmaxf(mn, ml[i].x);
+      const float a = fast_exp2(M - mn);
+      M = mn;
+      L *= a;
+      o *= a;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float b = fast_exp2(ml[i].x - mn);
+        L += ml[i].y * b;
+        o += x[i] * b;
+      }
+    }
   if constexpr (kShare > 1) {
     s_o[grp][threadIdx.x % L4] = o;
     if (e == 0) {
@@ -342,6 +380,60 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(MxAttnParams p, int pai
     *reinterpret_cast<f32x4 *>(static_cast<float *>(p.o_out) + gp * D + e) = o;
   }
   if (e == 0 && p.lse_out) p.lse_out[gp] = L == 0.f ? kNegInf : (M + __log2f(L)) * kLn2;
+}
+
+// The same for blocks of many pairs, which few workgroups share: PW pairs at a time of kMergePairs
+// of a block, whose parts are all on their way at once.  (8 pairs a workgroup, which most
+// workgroups spend finding out whose parts they merge: see attn_merge_kernel.)
+constexpr int kMergePairs = 32;
+template <int D, int PW>
+__global__ __launch_bounds__(256) void attn_merge_many_kernel(MxAttnParams p, int pairs, int pad) {
+  constexpr int L4 = D / 4, kTurns = kMergePairs / PW;
+  static_assert(PW * L4 == 256, "a group of lanes a pair");
+  const int n_pairs = p.mx.rows_per_seq * p.group, hkv = p.mx.n_kv_heads;
+  const int chunks = (min(pairs, n_pairs) + kMergePairs - 1) / kMergePairs;
+  const int sb = blockIdx.x / (chunks * hkv), rest = blockIdx.x - sb * (chunks * hkv);
+  const int h = rest / chunks, j0 = (rest - h * chunks) * kMergePairs + threadIdx.x / L4;
+  const int seq = sb / p.blocks_per_seq, rb = sb - seq * p.blocks_per_seq;
+  const int e = (threadIdx.x % L4) * 4;
+  if (rb * pairs + (rest - h * chunks) * kMergePairs >= n_pairs) return;
+  const MergeParts w = merge_parts(p, sb, h, pad);
+  if (w.w0 == w.w1) return;  // written by that workgroup
+  float M[kTurns], L[kTurns];
+  f32x4 o[kTurns];
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    M[i] = kMInit;
+    L[i] = 0.f;
+    o[i] = f32x4{};
+  }
+  for (int x = w.w0; x <= w.w1; ++x) {
+    const int64_t slot = (x == w.w0 ? w.first : 2 * (int64_t)x) * pairs + j0;
+    float2 ml[kTurns];
+    f32x4 y[kTurns];
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      ml[i] = p.part_ml[slot + i * PW];
+      y[i] = *reinterpret_cast<const f32x4 *>(p.part_o + (slot + i * PW) * D + e);
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const float mn = fmaxf(M[i], ml[i].x), a = fast_exp2(M[i] - mn), b = fast_exp2(ml[i].x - mn);
+      M[i] = mn;
+      L[i] = L[i] * a + ml[i].y * b;
+      o[i] = o[i] * a + y[i] * b;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int pair = rb * pairs + j0 + i * PW;
+    if (pair >= n_pairs) break;
+    o[i] *= L[i] == 0.f ? 0.f : 1.f / L[i];
+    const int64_t gp = ((int64_t)seq * p.mx.rows_per_seq + pair / p.group) * p.n_q_heads + h * p.group + pair % p.group;
+    *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
+        make_ushort4(f32_to_bf16(o[i][0]), f32_to_bf16(o[i][1]), f32_to_bf16(o[i][2]), f32_to_bf16(o[i][3]));
+    if (e == 0 && p.lse_out) p.lse_out[gp] = L[i] == 0.f ? kNegInf : (M[i] + __log2f(L[i])) * kLn2;
+  }
 }
 
 template <int D, int PW>
@@ -377,6 +469,12 @@ inline hipError_t launch_attn_merge(const MxAttnParams &p, const MxAttnShape &sh
   ProfScope ps(name, s);
   const int blocks = p.n_seqs * p.blocks_per_seq * p.mx.n_kv_heads;
   const bool few = sh.pairs <= 32 || p.n_workers > 4 * blocks;
+  if (pad && !few) {
+    const int grid = blocks * ((std::min(sh.pairs, p.mx.rows_per_seq * p.group) + kMergePairs - 1) / kMergePairs);
+    head_dim == 128 ? attn_merge_many_kernel<128, 8><<<grid, 256, 0, s>>>(p, sh.pairs, pad)
+                    : attn_merge_many_kernel<64, 16><<<grid, 256, 0, s>>>(p, sh.pairs, pad);
+    return hipGetLastError();
+  }
   if (head_dim == 128)
     launch_merge<128, 8>(p, sh, pad, blocks, few, bf16, s);
   else

@@ -36,6 +36,25 @@ class Store:
         self.desc = api.byte_desc(*self.dev, self.hq, self.ctx, None if self.contiguous else self.table.to(DEV),
                                 self.n_seqs)
 
+    def wide(self):
+        """A descriptor of the same cache with room for 2^18 tokens (pages that no row reaches): calls of many
+        pairs are made in blocks of 256 there."""
+        per = 2 ** 18 // self.page
+        table = torch.zeros(self.n_seqs, per, dtype=torch.int32)
+        table[:, :self.table.shape[1]] = self.table
+        return api.byte_desc(*self.dev, self.hq, 2 ** 18, table.to(DEV), self.n_seqs)
+
+    def many(self, r, dtype, desc):
+        """Whether a call with r rows per sequence takes blocks of 256 pairs."""
+        pairs = r * self.hq // self.hkv
+        return dtype == torch.bfloat16 and pairs > (64 if self.d == 128 else 128) and \
+            self.n_seqs * self.hkv * -(-pairs // 32) * desc.n_ctx >= 2 ** 18
+
+    def descs(self, r, dtype):
+        """The cache's descriptor, and the wide one if calls with r rows run otherwise there."""
+        wide = self.wide()
+        return [self.desc, wide] if self.many(r, dtype, wide) != self.many(r, dtype, self.desc) else [self.desc]
+
     def rows(self, s, n):
         """Keys and values of tokens 0 .. n - 1 of sequence s, float64."""
         pos = torch.arange(n)
@@ -55,14 +74,14 @@ class Store:
         self.cpu[which][int(self.table[s, t // self.page]), :, slot if which < 2 else slot // 16] = value
 
 
-def run(st, q, pos, lse=True, **kw):
+def run(st, q, pos, lse=True, desc=None, **kw):
     o = torch.full(q.shape, 9.0, dtype=q.dtype, device=DEV)
     l = torch.full(q.shape[:2], 9.0, device=DEV) if lse else None
-    api.conduit_attn_byte(st.desc, q.to(DEV), pos.to(DEV), o, lse_out=l, **kw)
+    api.conduit_attn_byte(desc or st.desc, q.to(DEV), pos.to(DEV), o, lse_out=l, **kw)
     return o.cpu(), None if l is None else l.cpu()
 
 
-def check(st, q, pos, o, lse, scale=None, rows=None):
+def check(st, q, pos, o, lse, scale=None, rows=None, desc=None):
     r = len(pos) // st.n_seqs
     for s in range(st.n_seqs):
         p = pos[s * r:(s + 1) * r]
@@ -72,7 +91,7 @@ def check(st, q, pos, o, lse, scale=None, rows=None):
         qq = q[s * r:(s + 1) * r][list(sel)]
         want = M.attention(qq, k, v, p[list(sel)], scale)
         bo, bl = B.attention_bounds(*want, n, st.d, q.dtype == torch.bfloat16)
-        if q.dtype == torch.bfloat16 and r * st.hq // st.hkv > 32:
+        if st.many(r, q.dtype, desc or st.desc):
             bo = bo + B.weight_floor(qq, k, v, st.factors(s, n), p[list(sel)], want[1], scale)
         go, gl = o[s * r:(s + 1) * r][list(sel)].double(), lse[s * r:(s + 1) * r][list(sel)].double()
         err = (go - want[0]).abs()
@@ -99,8 +118,9 @@ def test_attention(dtype, n_seqs, r, hq, hkv, d, ctx, page):
     q = queries(n_seqs * r, hq, d, dtype, r)
     pos = torch.randint(0, ctx, (n_seqs * r,), generator=g, dtype=torch.int32)
     pos[-1] = ctx - 1
-    o, lse = run(st, q, pos)
-    check(st, q, pos, o, lse)
+    for desc in st.descs(r, q.dtype):
+        o, lse = run(st, q, pos, desc=desc)
+        check(st, q, pos, o, lse, desc=desc)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -135,10 +155,11 @@ def test_empty_rows_and_sequences(dtype, ctx, r):
     pos[2, r // 2] = -2 ** 31                    # a padded row
     pos[3, r - 1] = 0
     pos = pos.flatten()
-    o, lse = run(st, q, pos)
-    check(st, q, pos, o, lse)
-    o, lse = run(st, q, torch.full_like(pos, -1))   # nothing at all
-    assert (o == 0).all() and (lse == -math.inf).all()
+    for desc in st.descs(r, q.dtype):
+        o, lse = run(st, q, pos, desc=desc)
+        check(st, q, pos, o, lse, desc=desc)
+        o, lse = run(st, q, torch.full_like(pos, -1), desc=desc)   # nothing at all
+        assert (o == 0).all() and (lse == -math.inf).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -150,8 +171,9 @@ def test_masked_keys_may_hold_anything(dtype, r, ctx):
     q = queries(r, 4, 128, dtype, 4)
     pos = torch.randint(0, ctx // 2, (r,), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
     pos[0] = ctx // 2
-    clean, clean_lse = run(st, q, pos)
-    check(st, q, pos, clean, clean_lse)
+    clean = [run(st, q, pos, desc=desc) for desc in st.descs(r, q.dtype)]
+    for desc, got in zip(st.descs(r, q.dtype), clean):
+        check(st, q, pos, *got, desc=desc)
     last = ctx // 2
     for t in range(last + 1, ctx):
         st.set(0, 0, t, (127, 255, 126, 3)[t % 4])
@@ -160,15 +182,17 @@ def test_masked_keys_may_hold_anything(dtype, r, ctx):
             st.set(2, 0, t, (255, 0, 246, 9)[t // 16 % 4])
             st.set(3, 0, t, (0, 255, 247, 246)[t // 16 % 4])
     st.upload()
-    o, lse = run(st, q, pos)
-    assert torch.equal(o, clean) and torch.equal(lse, clean_lse)
+    for desc, (co, cl) in zip(st.descs(r, q.dtype), clean):
+        o, lse = run(st, q, pos, desc=desc)
+        assert torch.equal(o, co) and torch.equal(lse, cl)
     nan_at = int(pos.sort().values[r // 2]) if r > 1 else last
     st.set(0, 0, nan_at, 0x7f)
     st.upload()
-    o, lse = run(st, q, pos)
     hit = pos >= nan_at
-    assert o[hit].isnan().all() and lse[hit].isnan().all()
-    assert torch.equal(o[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+    for desc, (co, cl) in zip(st.descs(r, q.dtype), clean):
+        o, lse = run(st, q, pos, desc=desc)
+        assert o[hit].isnan().all() and lse[hit].isnan().all()
+        assert torch.equal(o[~hit], co[~hit]) and torch.equal(lse[~hit], cl[~hit])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -185,6 +209,27 @@ def test_positions_past_the_cache(dtype):
     assert torch.equal(o2, o) and torch.equal(lse2, lse)
 
 
+@pytest.mark.parametrize("n_seqs,r,hq,hkv,d,ctx", [(1, 150, 4, 2, 128, 14011), (2, 60, 9, 3, 64, 7501)])
+def test_positions_past_a_cache_of_many_pairs(n_seqs, r, hq, hkv, d, ctx):
+    """The same with blocks of 256 pairs, whose last tile the cache ends in."""
+    st = Store(n_seqs, ctx, hq, hkv, d, seed=8)
+    assert st.many(r, torch.bfloat16, st.desc)
+    for i in (0, 1):                              # what is behind the last token is in no sequence
+        for s in range(n_seqs):
+            for t in range(ctx, -(-ctx // 64) * 64):
+                st.set(i, s, t, 0x7f)
+    st.upload()
+    q = queries(n_seqs * r, hq, d, "bf16", 5)
+    pos = torch.randint(0, ctx, (n_seqs * r,), generator=torch.Generator().manual_seed(6), dtype=torch.int32)
+    pos[::7] = ctx - 1
+    o, lse = run(st, q, pos)
+    check(st, q, pos, o, lse, rows=[0, 1, 6, 7, r - 1])
+    far = pos.clone()
+    far[::7], far[7] = ctx, 2 ** 31 - 1
+    o2, lse2 = run(st, q, far)
+    assert torch.equal(o2, o) and torch.equal(lse2, lse)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("r", [1, 3, 70])
 def test_sharp_and_rising_logits(dtype, r):
@@ -197,8 +242,9 @@ def test_sharp_and_rising_logits(dtype, r):
     q = queries(r, hq, d, dtype, 7, spread=3.0)
     pos = torch.linspace(ctx - 1, ctx // 3, r).to(torch.int32)
     for scale in (None, 0.3):
-        o, lse = run(st, q, pos, scale=scale)
-        check(st, q, pos, o, lse, scale=scale)
+        for desc in st.descs(r, q.dtype):
+            o, lse = run(st, q, pos, scale=scale, desc=desc)
+            check(st, q, pos, o, lse, scale=scale, desc=desc)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -227,7 +273,7 @@ def test_many_rows(dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("r", [1, 25])
+@pytest.mark.parametrize("r", [1, 25, 45])
 def test_a_workgroup_per_block(dtype, d, r):
     """More blocks than CUs, short caches: every block by one workgroup."""
     n = 300
@@ -260,7 +306,7 @@ def test_many_rows_of_small_heads():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("r", [2, 60])
+@pytest.mark.parametrize("r", [2, 90])
 def test_keys_past_a_row_hold_anything(dtype, d, r):
     """Rows of one block at tokens 95 and 600, whatever bytes follow token 95."""
     st = Store(1, 640, 4, 2, d, page=64, seed=23)
@@ -276,11 +322,12 @@ def test_keys_past_a_row_hold_anything(dtype, d, r):
     st.upload()
     pos = torch.tensor([95, 600] * (r // 2), dtype=torch.int32)
     q = queries(r, 4, d, dtype, 9)
-    o, lse = run(st, q, pos)
     want = M.attention(q[::2], k, v, pos[::2])
     bo, bl = B.attention_bounds(*want, 96, d, dtype == "bf16")
-    assert ((o[::2].double() - want[0]).abs() <= bo).all()
-    assert ((lse[::2].double() - want[1]).abs() <= bl).all()
+    for desc in st.descs(r, q.dtype):
+        o, lse = run(st, q, pos, desc=desc)
+        assert ((o[::2].double() - want[0]).abs() <= bo).all()
+        assert ((lse[::2].double() - want[1]).abs() <= bl).all()
 
 
 @pytest.mark.parametrize("n_seqs,hkv", [(9, 8), (60, 8), (64, 5), (65, 5)])
@@ -314,7 +361,7 @@ def test_many_sequences():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("r,ctx", [(1, 9000), (1, 200), (120, 3000)])
+@pytest.mark.parametrize("r,ctx", [(1, 9000), (1, 200), (120, 3000), (160, 8000)])
 def test_repeatable_and_workspace(dtype, r, ctx):
     """Bit for bit the same on repeated calls, on a workspace full of NaN, on one that
     another call has used, and without the log-sum-exp."""
@@ -335,7 +382,7 @@ def test_repeatable_and_workspace(dtype, r, ctx):
     assert torch.equal(run(st, q, pos, lse=False)[0], o)
 
 
-@pytest.mark.parametrize("r,ctx", [(1, 6000), (60, 1500)])
+@pytest.mark.parametrize("r,ctx", [(1, 6000), (60, 1500), (110, 9000)])
 def test_captured_calls(r, ctx):
     """Two captured calls that share one workspace, replayed with new positions and
     cache contents, eager calls in between."""
@@ -411,20 +458,22 @@ def test_value_scales_far_apart(dtype, r):
     st.upload()
     pos = torch.linspace(ctx - 1, 12, r).to(torch.int32)
     q = queries(r, hq, d, dtype, 3)
-    o, lse = run(st, q, pos)
-    check(st, q, pos, o, lse)
+    for desc in st.descs(r, q.dtype):
+        o, lse = run(st, q, pos, desc=desc)
+        check(st, q, pos, o, lse, desc=desc)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n_seqs,r", [(3, 40), (5, 3)])
+@pytest.mark.parametrize("n_seqs,r", [(3, 50), (5, 3)])
 def test_all_of_a_sequence(dtype, n_seqs, r):
     """Every row sees all of its sequence, as a text's rows an encoder's states."""
     st = Store(n_seqs, 777, 6, 2, 64, seed=41)
     length = torch.tensor([777, 1, 16, 300, 63][:n_seqs])
     pos = (length[:, None] - 1).expand(n_seqs, r).flatten().to(torch.int32)
     q = queries(n_seqs * r, 6, 64, dtype, 5)
-    o, lse = run(st, q, pos)
-    check(st, q, pos, o, lse)
+    for desc in st.descs(r, q.dtype):
+        o, lse = run(st, q, pos, desc=desc)
+        check(st, q, pos, o, lse, desc=desc)
 
 
 def test_outputs_are_rounded_once():
@@ -437,7 +486,7 @@ def test_outputs_are_rounded_once():
     for r in (1, 40):
         q = queries(r, 8, 128, "bf16", 6)
         pos = torch.full((r,), 5999, dtype=torch.int32)
-        o, _ = run(st, q, pos)
+        o, _ = run(st, q, pos, desc=st.descs(r, q.dtype)[-1])
         for i in range(min(r, 4)):
             want = M.attention(q[i:i + 1], k, v, pos[i:i + 1])[0]
             half = torch.ldexp(torch.ones((), dtype=torch.float64), torch.frexp(want)[1] - 9)
