@@ -667,8 +667,9 @@ typedef struct {
  * rows that attend to it are NaN there.
  *
  * pos       device int32 [n].  Within a sequence the positions in [0, n_ctx) ascend
- *           (a block that they come back to has meaningless contents); of rows with one
- *           position the last is held.  A row whose position is outside leaves the cache
+ *           (a block that they come back to, or that rows of two sequences go to in a
+ *           page that both have, has meaningless contents); of rows with one position
+ *           the last is held.  A row whose position is outside leaves the cache
  *           as it was (padded rows: -1); its q_out is still written.
  * n_held    nullable device int32 [n_seqs]: tokens that each sequence holds before the
  *           call, 0 .. n_held[s] - 1, are kept (values outside [0, n_ctx] are read as the
@@ -695,6 +696,11 @@ conduit_status conduit_load_byte(const conduit_kv_byte *cache, const int32_t *sr
  * example of a text's rows to an encoder's states of another length.  Among the values of
  * tokens that a row does not see NaN codes are harmless; among those that it sees they
  * count as NaN or as 0 (appends write none).
+ *
+ * Accuracy: products and sums are in fp32.  For bf16 tensors the probabilities enter the
+ * product with 11 bits or more; where a call has many (row, head) pairs for a KV head,
+ * they do so times the factor of their value block, p * 2^(s - 127), and are off by up to
+ * 2^-36 of the row's largest such product besides, times their code.
  * ------------------------------------------------------------------------ */
 size_t conduit_attn_byte_workspace_bytes(const conduit_kv_byte *cache, int32_t n, int32_t dtype);
 
