@@ -1,5 +1,32 @@
 // Causal attention over the 8-bit KV cache, gfx950.
 //
+//   o_i = sum_t p_it v_t / sum_t p_it,  p_it = exp(scale q_i k_t),  t = 0 .. pos_i
+// with keys and values code * 2^(s - 127), exact in bf16 (4 significant bits).  A call has
+// pairs (row, head): those of a sequence that share a KV head share its keys.  The work is
+// the list of all key steps of all (sequence, block of pairs, KV head); workgroups take equal
+// contiguous parts of it, and a second launch merges blocks that were cut (attn_steps.h).
+//
+// Few pairs (attn_byte_kernel): bound by reading the cache once, 2 (D + 1 / 16) bytes a key
+// and head.  Every wave has 32-key steps of its own in registers, in 16-byte loads that are
+// contiguous over the wave, the next step's in flight while this one's are used, and no
+// barrier before the end of its range.
+//   S^T = K Q^T  v_mfma_f32_16x16x32_bf16, 16 keys x 16 pairs: lane (key, g) has a quarter of
+//                the key's dims, decoded by v_cvt_scalef32_pk_bf16_fp8 with the block's
+//                scale; the queries are held in the same order of dims.
+//   softmax      online, in the log2 domain; a lane has one pair's column, so the running
+//                maximum and sum need no exchange between lanes unless the maximum rises by
+//                more than kSlack.
+//   O^T += V^T P^T  values decoded to bf16 in the wave's own LDS tile and read back with
+//                transposing reads; the probabilities are the other operand as they lie.
+// bf16 tensors: probabilities enter as two bf16 parts (2^-17 of each off; one part, 2^-9, would
+// show beside the output's one rounding); fp32: queries and probabilities as three exact parts.
+// The sum they are divided by is of the fp32 probabilities.
+// Measured (bf16, D = 128): 62 sequences of up to 32,768 tokens, 28 heads over 4, 1.06 GB: 190 us
+// and 5 to merge, 5.4 TB/s (a copy of 4 GiB: 4.5); one of 131,072, 32 heads over 8, 268 MB: 45 and 5;
+// 8 of up to 8,211 with 5 rows, 76 MB: 21 and 5, which is mostly the chain of loads a
+// workgroup begins with (positions, page, codes) for 4 steps of its own.
+//
+// Many pairs (attn_byte_many_kernel): bound by the matrix products.  See there.
 #include <type_traits>
 
 #include "attn_steps.h"
@@ -63,14 +90,14 @@ constexpr int waves_per_simd(int D, int MT, int NS) {
   return D == 128 ? 2 : (MT == 1 ? (NS == 1 ? 4 : 3) : NS == 1 ? 3 : 2);
 }
 // Pairs of a block with few pairs: 32 read the cache once for twice as many, but
-// fp32 rows of 128 dims would leave registers for one wave per SIMD only (1,500
-// rows over 16k tokens: 32 pairs 1,094 us, 16 pairs 804 us).
+// fp32 rows of 128 dims would leave registers for one wave per SIMD only (28 heads over 4, 32 and 16
+// pairs: 200 rows over 4,096 tokens 70 and 57 us, 64 sequences of 4,096 with 8 rows 156 and 122).
 constexpr int few_pairs(int D, int64_t pairs, bool bf16) { return pairs <= 16 || (D == 128 && !bf16) ? 16 : 32; }
 
 // MT: groups of 16 pairs of a block.  NS: exact bf16 parts of queries (1: bf16
 // tensors, 3: fp32).  W: waves of a workgroup, 4, or 8 for a
-// workgroup per block on up to 256 blocks (64 sequences of 2,048 keys: 4 waves 20
-// us, 8 waves 16 us; 256 of 512, which leave the CUs several blocks each: 16 and 24 us).
+// workgroup per block on up to 256 blocks (64 sequences of up to 2,048 keys, 4 KV heads: 4 waves 26
+// us, 8 waves 20; 256 of up to 512, which leave the CUs several blocks each: 21 and 29).
 template <int D, int MT, int NS, int W>
 __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_kernel(MxAttnParams p) {
   constexpr int kWaves = W, kStep = W * kWaveKeys;
@@ -253,8 +280,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
       wave_lds_fence();
     };
 
-    // Two register sets take turns: a step is loaded while the one before it is used
-    // (two steps ahead gain nothing), its page looked up one step earlier still.
+    // Two register sets take turns: a step is loaded while the one before it is used,
+    // its page looked up one step earlier still.
     {
       const int end = min(most, last * kStep);  // (last * kStep < n_ctx + kStep <= 2^30 + kStep)
       auto turn = [&](Step<D> &now, Step<D> &next) __attribute__((always_inline)) {
@@ -330,7 +357,36 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
   }
 }
 
-// Many pairs per KV head: keys and values are decoded once for 256 pairs into LDS.
+// Many pairs per KV head (the rows of a refresh, a text's rows over an encoder's states): keys
+// and values are decoded once for 256 pairs, 32 a wave, into a ring of four tiles of 64 keys in LDS.
+//   S^T = K Q^T     v_mfma_f32_32x32x16_bf16, keys as bf16 with their scale.
+//   O^T += V^T W^T  v_mfma_f32_32x32x16_f16: values as their bare codes (exact in fp16), and the
+//                   block's scale goes into the weight, as part of the exponent that the
+//                   softmax computes anyway:  w = 2^(x + log2 f - M + kHead)  for the score x
+//                   (log2 units) and the factor f of its value block, over the running maximum M
+//                   of x + log2 f.  A weight is rounded once, by up to 2^-12 of it, where one
+//                   bf16 part would lose 2^-9 and two would double the second product; weights
+//                   below fp16's normal numbers are off by 2^-25, 2^-36 of the largest.
+//   l += 2^(x - m)  the sum, in fp32 over a running maximum m of its own: two exponents a
+//                   16-key block then share the exponential, e = 2^(x - at), at = M - kHead - log2 f, and
+//                   what a block adds to l is put right by 2^(at - m) once.  Where a block's factor is
+//                   so small that e would leave fp32 (at > m + kFar) at is m + kFar: weights of such
+//                   a block, below 2^(kManySlack - kFar), are 0 in fp16 either way.
+// Both maxima move when a step exceeds them by more than kManySlack: weights stay below
+// 2^(kHead + kManySlack) = 2^15, and sums lose nothing.
+//
+// A step of 32 keys is 2 C slots of one product each, with a share of the vector work of the
+// softmax (of the scores computed one step before), an operand read from LDS for C slots
+// later, and in turn a tile's loads, decoding and LDS writes.  sched_barrier and the
+// empty statements keep each slot's work in it; the compiler otherwise gathers the exponentials and
+// the products apart.
+//
+// What bounds it: the product of 32 x 32 x 16 takes 13.8 ns a SIMD on zeros and 21 on random
+// numbers (1.6 PFLOP/s: the chip lowers its clock), 27.6 with the vector work that a slot needs here. A
+// tile takes 2.06 us at D = 128 (64 keys, 256 pairs a CU: 1.04 PFLOP/s over the chip) and 1.39 at
+// D = 64.  64 pairs a wave on one wave a SIMD take as long (2.03 to 2.06; 1.50 at D = 64), so do slots that
+// lag the waves behind one another (2.06 to 2.10), and keys and values decoded
+// by every wave for itself take 620 us for 1,638 rows over 17,024 keys where this takes 232.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr int kManyWaves = 8;
@@ -772,10 +828,12 @@ MxAttnShape byte_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_he
   // Workgroups share the steps out evenly, for a second launch that merges, from
   // this many steps of a block on (and while the parts' list fits LDS): fewer are
   // done sooner by a workgroup per block, and the more blocks there are the less
-  // there is to even out.  One sequence of 4 KV heads: 1,024 keys 9 us by block,
-  // 11 us shared; 2,200 keys 14 and 11 us.  64 sequences of up to 2,048: 15 and 20
-  // us.  256 of up to 4,096: 75 and 84 us, of up to 8,192: 144 and 140 us.
-  const int64_t from = blocks < 256 ? 8 : blocks < 1024 ? 16 : 32;
+  // there is to even out.  4 KV heads, by block and shared: one sequence of 512 keys 8 and 11
+  // us, of 1,024 11 and 11, of 2,200 18 and 11; 64 of up to 2,048 20 and 23, of 4,096 34 and 39,
+  // of 32,768 (shared) 195; 80 of up to 6,000 70 and 58; 256 of up to 4,096 126 and 134, of
+  // 8,192 230 and 219.  Blocks of 256 pairs: 192 of 2,048 keys 71 and 86, 64 of 2,048 67
+  // and 53, 256 of 4,096 (as even as can be) 143 and 153.
+  const int64_t from = blocks < 256 ? 8 : many && blocks < 1024 ? 16 : 32;
   // (The merge has up to L.pairs workgroups of 256 threads a block, fewer than 2^32.)
   if (steps > from && n_sb <= kMaxSeqBlocks && 2 * blocks * (steps + kManyPad) < INT32_MAX &&
       blocks * L.pairs < 1 << 24)
