@@ -22,7 +22,7 @@
 // show beside the output's one rounding); fp32: queries and probabilities as three exact parts.
 // The sum they are divided by is of the fp32 probabilities.
 // Measured (bf16, D = 128): 62 sequences of up to 32,768 tokens, 28 heads over 4, 1.06 GB: 190 us
-// and 5 to merge, 5.4 TB/s (a copy of 4 GiB: 4.5); one of 131,072, 32 heads over 8, 268 MB: 45 and 5;
+// and 5 to merge, 5.5 TB/s (a copy of 4 GiB: 4.5); one of 131,072, 32 heads over 8, 268 MB: 51 and 5;
 // 8 of up to 8,211 with 5 rows, 76 MB: 21 and 5, which is mostly the chain of loads a
 // workgroup begins with (positions, page, codes) for 4 steps of its own.
 //
