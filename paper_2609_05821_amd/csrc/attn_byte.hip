@@ -745,13 +745,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
     l += __shfl_xor(l, 32, 64);
     if (j0 < n_pairs) {
       const int64_t gp = (row_base + pair / G) * p.n_q_heads + h * G + pair % G;
-      const float unit = fast_exp2(M - m - kHead), inv = l == 0.f ? 0.f : unit / l;
+      // What a weight of 1 stands for, in two equal factors: with the smallest value scales 2^-128.
+      const float unit = fast_exp2(0.5f * (M - m - kHead)), inv = l == 0.f ? 0.f : unit / l;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int e = 32 * dt + 8 * i + 4 * hh;
-          const f32x4 y = {o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+          const f32x4 y = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]} * unit;
           if (whole)
             *reinterpret_cast<ushort4 *>(static_cast<u16 *>(p.o_out) + gp * D + e) =
                 make_ushort4(f32_to_bf16(y[0] * inv), f32_to_bf16(y[1] * inv), f32_to_bf16(y[2] * inv),
