@@ -697,8 +697,7 @@ conduit_status conduit_load_byte(const conduit_kv_byte *cache, const int32_t *sr
  * tokens that a row does not see NaN codes are harmless; among those that it sees they
  * count as NaN or as 0 (appends write none).
  *
- * Accuracy: products and sums are in fp32, and sums are divided last, so that values above
- * about 2^127 / (2^8 keys) may become infinite in them.  For bf16 tensors the probabilities enter the
+ * Accuracy: products and sums are in fp32.  For bf16 tensors the probabilities enter the
  * product with 11 bits or more; where a call has many (row, head) pairs for a KV head,
  * they do so times the factor of their value block, p * 2^(s - 127), and are off by up to
  * 2^-36 of the row's largest such product besides, times their code.

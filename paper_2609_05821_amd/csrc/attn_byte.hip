@@ -18,7 +18,7 @@
 //                more than kSlack.
 //   O^T += V^T P^T  values decoded to bf16 in the wave's own LDS tile and read back with
 //                transposing reads; the probabilities are the other operand as they lie.
-// bf16 tensors: probabilities enter as two bf16 parts (2^-17 of each off; one part, 2^-9, would
+// bf16 tensors: probabilities enter as two bf16 parts (2^-17 of each off; one part, 2^-8, would
 // show beside the output's one rounding); fp32: queries and probabilities as three exact parts.
 // The sum they are divided by is of the fp32 probabilities.
 // Measured (bf16, D = 128): 62 sequences of up to 32,768 tokens, 28 heads over 4, 1.06 GB: 190 us
@@ -364,8 +364,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
 //                   block's scale goes into the weight, as part of the exponent that the
 //                   softmax computes anyway:  w = 2^(x + log2 f - M + kHead)  for the score x
 //                   (log2 units) and the factor f of its value block, over the running maximum M
-//                   of x + log2 f.  A weight is rounded once, by up to 2^-12 of it, where one
-//                   bf16 part would lose 2^-9 and two would double the second product; weights
+//                   of x + log2 f.  A weight is rounded once, by up to 2^-11 of it, where one
+//                   bf16 part would lose 2^-8 and two would double the second product; weights
 //                   below fp16's normal numbers are off by 2^-25, 2^-36 of the largest.
 //   l += 2^(x - m)  the sum, in fp32 over a running maximum m of its own: two exponents a
 //                   16-key block then share the exponential, e = 2^(x - at), at = M - kHead - log2 f, and

@@ -122,11 +122,12 @@ def attention_bounds(o, lse, av, mag, n_keys, d, bf16):
     """Elementwise bounds of the kernel's error (o, lse, av, mag of mx_oracle.attention).
     Logits: d products added in fp32, then the scale and the exponent's argument, each
     at most 2^-24 of mag; twice (numerator and denominator).  Exponential 2^-22.  For bf16
-    tensors the probabilities enter the product rounded to 2^-12 of each or better.  Sums of
+    tensors the probabilities enter the product as fp16 numbers or better: of a number in [2^e, 2^(e+1)) fp16 keeps
+    11 bits, its steps are 2^(e-10), and half a step is up to 2^-11 of the number.  Sums of
     n_keys terms in fp32 (numerator and denominator), merges of parts within 64 more
     roundings.  Output: one rounding, half a step."""
     es = 2 * (d + 8) * 2.0 ** -24 * mag + 2 * 2.0 ** -22 + 2 * (n_keys + 64) * 2.0 ** -24
-    bo = (es + (2.0 ** -12 if bf16 else 0.0))[..., None] * av + (2.0 ** -8 if bf16 else 2.0 ** -24) * o.abs() + 1e-30
+    bo = (es + (2.0 ** -11 if bf16 else 0.0))[..., None] * av + (2.0 ** -8 if bf16 else 2.0 ** -24) * o.abs() + 1e-30
     bl = es + 2.0 ** -21 * lse.abs().nan_to_num(0.0, 0.0, 0.0) + 2.0 ** -22
     return bo, bl
 

@@ -147,7 +147,7 @@ def test_stored_image_moved_and_scored():
     want = M.attention(q.cpu(), lk.cpu().double(), lv.cpu().double(), rows.cpu())
     bo, _ = B.attention_bounds(*want, n, D, True)
     assert ((o8.cpu().double() - want[0]).abs() <= bo).all()
-    # (16-bit attention rounds its probabilities to bf16, 2^-8 of each where this one has 2^-12, so its own bound is
+    # (16-bit attention rounds its probabilities to bf16, 2^-8 of each where this one has 2^-11, so its own bound is
     # wider; both are off by their bounds at most)
     b16, _ = M.attention_bounds(*want, n, D, True)
     assert ((o8.cpu().double() - o16.cpu().double()).abs() <= bo + b16).all()
