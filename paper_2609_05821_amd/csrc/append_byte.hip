@@ -32,12 +32,17 @@ namespace {
 // the other the values.
 constexpr int kMaxHeads = 4;
 constexpr int kMaxWaves = 2 * kMaxHeads;
-// Rows of a window.  16 where there are many; with few, 4 keep the chip busy and a window's
-// short runs are taken side by side (1,638 rows here and there, windows of 1, 2, 4 and 8: 18, 16, 13 and 17
-// us; 6,553 rows 30 us with windows of 4 and 55 with 16, but 65,536 rows of a document 67 us with
-// 16 and 80 with the code that takes short runs side by side, whose registers leave fewer waves).
+// Rows of a window.  Fewer keep the chip busy with few rows (rows that continue a run leave at once) and take
+// their runs of one or two rows side by side, a wave each, before the longer ones; windows of 16 have
+// workgroups of their own for such runs; with many rows these are left out, and the code for them, whose
+// registers leave fewer waves.  Rows of a prompt, and rows here and there over ten times as many tokens,
+// keys, values and 28 query heads over 4, in us:
+//   rows                                    1,638      2,200      4,000      8,000      20,000
+//   windows of 4                            13   14    18   18    28   28    52   58
+//   16, short runs apart                    12   21    12   22    18   23    32   46    88  115
+//   16, short runs like others                                                          74  119
 constexpr int kWindow = 16, kWindowFew = 4;
-constexpr int kWindowFrom = 8192;
+constexpr int kWindowFrom = 2048, kManyFrom = 8192;
 // Rows of a workgroup that turns queries, and from how many rows on.
 constexpr int kQueryRows = 2, kQueryRowsFrom = 512;
 
@@ -189,11 +194,12 @@ __device__ __forceinline__ void turn_queries(const RowParams &p, int row0, int n
   }
 }
 
-// Workgroups [0, n_runs): windows of rows, for up to 4 KV heads each.  The others: queries.
+// Workgroups [0, n_runs): windows of rows, for up to 4 KV heads each.  The next n_brief: the windows' runs of
+// one or two rows (0: they are among the first).  The others: queries.
 // BRIEF: with a path of their own for runs of one or two rows.
 template <typename T, int D, bool BRIEF>
 __global__ __launch_bounds__(64 * kMaxWaves, BRIEF || (sizeof(T) == 4 && D == 128) ? 4 : 6)
-void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_rows) {
+void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int n_brief, int query_rows) {
   constexpr int LR = D / 16;        // lanes of a token's head
   constexpr int RP = 64 / LR;       // tokens that the lanes hold
   constexpr int SL = kByteBlock / RP;  // tokens of a lane
@@ -201,14 +207,15 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_ro
   __shared__ int s_row[kMaxWaves][kByteBlock];  // the run's row of each token of the block, or -1
   __shared__ uint64_t s_bad[2][kMaxWaves][SL];  // lanes whose token is not finite there
   const RowParams &p = a.rows;
-  if ((int)blockIdx.x >= n_runs) {
-    const int row0 = ((int)blockIdx.x - n_runs) * query_rows;
+  if ((int)blockIdx.x >= n_runs + n_brief) {
+    const int row0 = ((int)blockIdx.x - n_runs - n_brief) * query_rows;
     turn_queries<T, D>(p, row0, min(query_rows, p.n - row0), s_cs);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int heads = blockDim.x >> 7, head_groups = (p.n_kv_heads + heads - 1) / heads;
-  const int row0 = (int)blockIdx.x / head_groups * window;
+  const bool for_brief = BRIEF && (int)blockIdx.x >= n_runs;
+  const int row0 = (for_brief ? (int)blockIdx.x - n_runs : (int)blockIdx.x / head_groups) * window;
   const int h = (int)blockIdx.x % head_groups * heads + (wave >> 1);
   const bool keys = !(wave & 1);
   const int r = p.mx.rows_per_seq, half = p.rope.half;
@@ -263,6 +270,15 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_ro
     int seq, token0, page;
     uint32_t written, kept;
   };
+  // Where the run lies whose first row is lane `first`'s, and what its block keeps.
+  auto place_run = [&](Run &x, int first) __attribute__((always_inline)) {
+    x.token0 = x.out ? 0 : __builtin_amdgcn_readlane(block, first) * kByteBlock;
+    x.page = __builtin_amdgcn_readlane(page_at, first);
+    const int held = x.out          ? 0
+                     : a.n_held ? min(max(__builtin_amdgcn_readlane(held_at, first), 0), p.mx.n_ctx)
+                                    : x.token0 + 31 - __builtin_clz(x.written);
+    x.kept = ~x.written & ((1u << min(max(held - x.token0, 0), kByteBlock)) - 1);
+  };
   auto run_of = [&](int first) __attribute__((always_inline)) {
     Run x;
     x.out = outs >> first & 1;
@@ -293,12 +309,7 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_ro
       wave_lds_fence();
     }
     x.written = (uint32_t)__ballot(rows[lane & (kByteBlock - 1)] >= 0) & 0xffffu;
-    x.token0 = x.out ? 0 : run_block * kByteBlock;
-    x.page = __builtin_amdgcn_readlane(page_at, first);
-    const int held = x.out          ? 0
-                     : a.n_held ? min(max(__builtin_amdgcn_readlane(held_at, first), 0), p.mx.n_ctx)
-                                    : x.token0 + 31 - __builtin_clz(x.written);
-    x.kept = ~x.written & ((1u << min(max(held - x.token0, 0), kByteBlock)) - 1);
+    place_run(x, first);
     return x;
   };
   // Codes and scale byte of a run's block for one head.
@@ -336,26 +347,35 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_ro
 
   // Runs of one or two rows (and rows that are left out): a wave each, side by side.
   uint64_t brief = 0;
+  int second = lane;  // the lane of the run's other row
   if constexpr (BRIEF) {
     const uint64_t all_leaders = __ballot(live && !continues), later = lane < 63 ? all_leaders >> (lane + 1) : 0;
     const int next = later ? lane + 1 + __builtin_ctzll(later) : 64;
     const uint64_t own = lives >> lane & (next < 64 ? (1ull << (next - lane)) - 1 : ~0ull);
+    if (__builtin_popcountll(own) == 2) second = lane + 63 - __builtin_clzll(own);
     brief = (__ballot(__builtin_popcountll(own) <= 2 && (next < 64 || row0 + 64 >= p.n)) & leaders) | outs;
   }
-  if (BRIEF && (int)blockIdx.x % head_groups == 0) {  // (one workgroup for all heads here)
+  if (BRIEF && (n_brief ? for_brief : (int)blockIdx.x % head_groups == 0)) {  // (one workgroup for all heads)
     constexpr int kUnits = 64 / LR;  // heads' keys or values side by side
     const int n_units = 2 * p.n_kv_heads;
     f64x2 *cs = s_cs + 2 * wave * half;
     uint64_t todo = brief;
     for (int skip = wave; skip > 0; --skip) todo &= todo - 1;
     while (todo) {
-      const Run x = run_of(__builtin_ctzll(todo));
+      const int first = __builtin_ctzll(todo);
+      Run x;
+      x.out = outs >> first & 1;
       for (int skip = 2 * heads; skip > 0; --skip) todo &= todo - 1;
-      int token[2], row[2];  // (one: the same twice)
-      token[0] = __builtin_ctz(x.written);
-      token[1] = 31 - __builtin_clz(x.written);
-#pragma unroll
-      for (int y = 0; y < 2; ++y) row[y] = __builtin_amdgcn_readfirstlane(rows[token[y]]);
+      // (one row, or the later of two with one position: the same twice)
+      const int other = x.out ? first : __builtin_amdgcn_readlane(second, first);
+      int token[2] = {0, 0}, row[2] = {row0 + first, row0 + other};
+      if (!x.out) {
+        token[0] = __builtin_amdgcn_readlane(at, first) & (kByteBlock - 1);
+        token[1] = __builtin_amdgcn_readlane(at, other) & (kByteBlock - 1);
+        if (token[0] == token[1]) row[0] = row[1];
+      }
+      x.written = 1u << token[0] | 1u << token[1];
+      place_run(x, first);
       for (int u0 = 0; u0 < n_units; u0 += kUnits) {
         const int u = min(u0 + lane / LR, n_units - 1), head = u >> 1;
         const bool k = !(u & 1), valid = u0 + lane / LR < n_units;
@@ -432,6 +452,7 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_ro
       }
     }
   }
+  if (for_brief) return;
   leaders &= ~brief;
   outs &= ~brief;
 
@@ -531,15 +552,16 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int query_ro
 template <typename T, int D>
 void launch(const ByteAppendParams &a, hipStream_t s) {
   const RowParams &p = a.rows;
-  const bool many = p.n >= kWindowFrom;
-  const int window = many ? kWindow : kWindowFew, query_rows = p.n >= kQueryRowsFrom ? kQueryRows : 1;
+  const bool many = p.n >= kManyFrom;
+  const int window = p.n >= kWindowFrom ? kWindow : kWindowFew, query_rows = p.n >= kQueryRowsFrom ? kQueryRows : 1;
   const int heads = std::min(p.n_kv_heads, kMaxHeads), groups = (p.n_kv_heads + heads - 1) / heads;
-  const int n_runs = (p.n + window - 1) / window * groups;
-  const int grid = n_runs + (p.n_q_heads ? (p.n + query_rows - 1) / query_rows : 0);
+  const int windows = (p.n + window - 1) / window, n_runs = windows * groups;
+  const int n_brief = many || window == kWindowFew ? 0 : windows;
+  const int grid = n_runs + n_brief + (p.n_q_heads ? (p.n + query_rows - 1) / query_rows : 0);
   if (many)
-    append_byte_kernel<T, D, false><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, query_rows);
+    append_byte_kernel<T, D, false><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, n_brief, query_rows);
   else
-    append_byte_kernel<T, D, true><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, query_rows);
+    append_byte_kernel<T, D, true><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, n_brief, query_rows);
 }
 
 }  // namespace

@@ -61,7 +61,14 @@ def append(c, pos, k, v, n_held=None, rope=None, rp=None, held=True, **kw):
     wk, wv = c.want.append(pos, kt, v.cpu(), n_held)
     c.check()
     if held:
+        # a row whose position a later row of its sequence has is not written
+        r, last = len(pos) // c.want.table.shape[0], {}
+        for i, t in enumerate(pos.tolist()):
+            if 0 <= t < c.ctx:
+                last[(i // r, t)] = i
+        gone = torch.tensor([0 <= t < c.ctx and last[(i // r, t)] != i for i, t in enumerate(pos.tolist())])
         for got, want in ((ko, wk), (vo, wv)):
+            want[gone] = 9.0
             got, want = got.cpu().double(), want.float().to(k.dtype).double()
             assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
     return wk, wv
@@ -162,7 +169,7 @@ def test_rows_left_out(gaps):
     append(c, pos, k, v * 9, held=False, n_held=torch.tensor([30, 400], dtype=torch.int32))
 
 
-@pytest.mark.parametrize("n", [511, 512, 4500, 8191, 8192, 10000])
+@pytest.mark.parametrize("n", [511, 512, 2047, 2050, 4500, 8191, 8192, 10000])
 @pytest.mark.parametrize("hkv", [1, 5])
 def test_many_rows(n, hkv):
     """Either side of the number of rows from which workgroups take 16 each; first positions
@@ -184,7 +191,8 @@ def test_many_rows(n, hkv):
     assert torch.equal(q_out, want)
 
 
-@pytest.mark.parametrize("n,ctx,hkv,d", [(900, 9000, 2, 64), (800, 1100, 6, 128), (8300, 30000, 1, 64)])
+@pytest.mark.parametrize("n,ctx,hkv,d", [(900, 9000, 2, 64), (800, 1100, 6, 128), (2600, 20000, 6, 128),
+                                           (4100, 6000, 5, 64), (8300, 30000, 1, 64)])
 def test_scattered_rows_in_windows(n, ctx, hkv, d):
     """Windows that begin many runs, short and long ones, runs that begin in one window and end
     in the next; more heads than a workgroup takes."""
@@ -194,6 +202,24 @@ def test_scattered_rows_in_windows(n, ctx, hkv, d):
     _, k, v = new_rows(n, hkv, hkv, d, "bf16", 3)
     rope, rp = rope_of(d // 4, 1, 0), torch.randint(0, 9000, (1, n), generator=g, dtype=torch.int32).to(DEV)
     append(c, pos, k, v * 5, n_held=torch.tensor([ctx - 100], dtype=torch.int32), rope=rope, rp=rp)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_seqs,r,ctx,hkv", [(3, 200, 700, 3), (3, 700, 3000, 5), (1, 2100, 2500, 2),
+                                              (40, 60, 300, 4)])
+def test_windows_of_every_kind_of_run(dtype, n_seqs, r, ctx, hkv):
+    """Rows here and there, some of them twice, one in four left out, in windows of 4 and of 16 rows."""
+    g = torch.Generator().manual_seed(r)
+    c = Cache(n_seqs, ctx, hkv, hkv, 64, seed=r)
+    pos = torch.randint(0, ctx, (n_seqs, r), generator=g).sort(1).values
+    pos[torch.rand(n_seqs, r, generator=g) < 0.25] = -1
+    pos = pos.flatten().to(torch.int32)
+    _, k, v = new_rows(n_seqs * r, hkv, hkv, 64, dtype, 4)
+    held = torch.randint(0, ctx, (n_seqs,), generator=g, dtype=torch.int32)
+    rope, rp = rope_of(16, 1, 0), torch.randint(0, 99, (1, n_seqs * r), generator=g, dtype=torch.int32).to(DEV)
+    append(c, pos, k, v * 3, n_held=held, rope=rope, rp=rp)
+    pos[1:][pos[1:] == pos[:-1]] = -1
+    append(c, pos, k * 2, v, n_held=held, rope=rope, rp=rp)
 
 
 def test_the_last_of_rows_with_one_position():
@@ -225,7 +251,8 @@ def test_hard_values(dtype):
     k, v = (t.to(DT[dtype]).to(DEV) for t in x)
     c = Cache(1, n + 30, hkv, hkv, d, seed=2, lo=0, hi=256)          # scale bytes that no append writes, too
     append(c, torch.arange(n, dtype=torch.int32), k, v)
-    append(c, torch.arange(0, n, 3, dtype=torch.int32), k[::3] * 0.5, v[::3], n_held=torch.tensor([n], dtype=torch.int32))
+    third = torch.arange(0, n, 3, dtype=torch.int32)
+    append(c, third, k[::3] * 0.5, v[::3], n_held=torch.tensor([n], dtype=torch.int32))
 
 
 def test_largest_scales_meet_smallest():
