@@ -41,8 +41,9 @@ constexpr int kMaxWaves = 2 * kMaxHeads;
 //   windows of 4                            13   14    18   18    28   28    52   58
 //   16, short runs apart                    12   21    12   22    18   23    32   46    88  115
 //   16, short runs like others                                                          74  119
-constexpr int kWindow = 16, kWindowFew = 4;
-constexpr int kWindowFrom = 2048, kManyFrom = 8192;
+// (100 rows in windows of 2 and of 4: 9 10 and 10 11; 400: 9 11 and 10 12; 1,000: 14 13 and 10 12.)
+constexpr int kWindow = 16, kWindowFew = 4, kWindowLeast = 2;
+constexpr int kWindowFewFrom = 512, kWindowFrom = 2048, kManyFrom = 8192;
 // Rows of a workgroup that turns queries, and from how many rows on.
 constexpr int kQueryRows = 2, kQueryRowsFrom = 512;
 
@@ -553,10 +554,11 @@ template <typename T, int D>
 void launch(const ByteAppendParams &a, hipStream_t s) {
   const RowParams &p = a.rows;
   const bool many = p.n >= kManyFrom;
-  const int window = p.n >= kWindowFrom ? kWindow : kWindowFew, query_rows = p.n >= kQueryRowsFrom ? kQueryRows : 1;
+  const int window = p.n >= kWindowFrom ? kWindow : p.n >= kWindowFewFrom ? kWindowFew : kWindowLeast;
+  const int query_rows = p.n >= kQueryRowsFrom ? kQueryRows : 1;
   const int heads = std::min(p.n_kv_heads, kMaxHeads), groups = (p.n_kv_heads + heads - 1) / heads;
   const int windows = (p.n + window - 1) / window, n_runs = windows * groups;
-  const int n_brief = many || window == kWindowFew ? 0 : windows;
+  const int n_brief = many || window < kWindow ? 0 : windows;
   const int grid = n_runs + n_brief + (p.n_q_heads ? (p.n + query_rows - 1) / query_rows : 0);
   if (many)
     append_byte_kernel<T, D, false><<<grid, 128 * heads, 0, s>>>(a, window, n_runs, n_brief, query_rows);
