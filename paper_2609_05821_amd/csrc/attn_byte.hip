@@ -472,37 +472,39 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
       asm("" : "+v"(zero));
       x.vs = *reinterpret_cast<const uint32_t *>(c.v_scale + at.scales + zero);
     };
-    // The first two tiles are on their way before anything else is.
-    Raw raw0, raw;
-    Place at2;
-    int entry3;
-    {
-      int entry[3];
+    // Page entries first, queries and positions behind them: tiles are asked for as soon as
+    // the entries are there, and the rest arrives meanwhile.
+    int entry[3], entry3;
 #pragma unroll
-      for (int i = 0; i < 3; ++i) entry[i] = page_entry(pages, index(sg.first + i));
-      entry3 = page_entry(pages, index(sg.first + 3));
-      const Place at0 = place(sg.first, entry[0]), at1 = place(sg.first + 1, entry[1]);
-      at2 = place(sg.first + 2, entry[2]);
-      load_keys(at0, raw0);
-      load_values(at0, raw0);
-      load_keys(at1, raw);
-      load_values(at1, raw);
-    }
+    for (int i = 0; i < 3; ++i) entry[i] = page_entry(pages, index(sg.first + i));
+    entry3 = page_entry(pages, index(sg.first + 3));
 
     // The lane's pair: its query and how many keys it sees (one that is not there sees all).
     const int j0 = 32 * wave + col, pair = block0 + j0;
     bf16x8 q[C];
-    int seen = INT32_MAX, most = 0;
+    int pos = 0;
 #pragma unroll
     for (int x = 0; x < C; ++x) q[x] = bf16x8{};
     if (j0 < n_pairs) {
       const int row = pair / G;
-      seen = most = keys_seen(p.pos[row_base + row], c.n_ctx);
+      pos = p.pos[row_base + row];
       const u16 *at =
           static_cast<const u16 *>(p.q) + ((row_base + row) * p.n_q_heads + h * G + pair % G) * D + 8 * hh;
 #pragma unroll
       for (int x = 0; x < C; ++x) q[x] = as_bf16x8(ld16(at + 16 * x));
     }
+    __builtin_amdgcn_sched_barrier(0);
+
+    Raw raw0, raw;
+    const Place at0 = place(sg.first, entry[0]), at1 = place(sg.first + 1, entry[1]);
+    const Place at2 = place(sg.first + 2, entry[2]);
+    load_keys(at0, raw0);
+    load_values(at0, raw0);
+    load_keys(at1, raw);
+    load_values(at1, raw);
+    __builtin_amdgcn_sched_barrier(0);
+    const int seen = j0 < n_pairs ? keys_seen(pos, c.n_ctx) : INT32_MAX;
+    int most = j0 < n_pairs ? seen : 0;
     most = __builtin_amdgcn_readfirstlane(wave_max_i(most));
     const int least = __builtin_amdgcn_readfirstlane(wave_min_i(seen));
     __syncthreads();
@@ -713,9 +715,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
         }
         settle(y, 32 * s + 32, svn);
       };
-      // (a wave whose rows end before the block's goes on: masked, and rarely by more than
-      // a few tiles)
-      for (int tile = sg.first; tile < last; ++tile) {
+      // A wave without pairs, or past its rows' last key, has no products left: it goes on with its share
+      // of the tiles (64 sequences of 4,096 keys with 96 pairs: 133 us with its masked products, 96 without).
+      const int own = min(last, (most + kTileKeys - 1) / kTileKeys);
+      int tile = sg.first;
+      for (; tile < own; ++tile) {
         clean(tile + 2, raw);
         scale_of_step(vs0, 1, sv1);
         // Registers are loaded anew once they are in LDS: a tile ahead of their use.
@@ -738,10 +742,22 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
         vs1 = vs2;
         __syncthreads();
       }
+      for (; tile < last; ++tile) {
+        clean(tile + 2, raw);
+        put_keys(tile + 2, raw);
+        put_values(tile + 2, raw);
+        const Place at3 = place(tile + 3, entry3);
+        load_keys(at3, raw);
+        load_values(at3, raw);
+        entry3 = page_entry(pages, index(tile + 4));
+        __syncthreads();
+      }
     }
 
     const bool whole = !p.n_workers || (sg.first == 0 && sg.last == sg.steps);
     const int slot = 2 * blockIdx.x + (part.t - sg.listed == part0 ? 0 : 1);
+    int row_at = j0;  // (hidden: addresses made of it before the first segment would cost registers throughout)
+    asm volatile("" : "+v"(row_at));
     l += __shfl_xor(l, 32, 64);
     if (j0 < n_pairs) {
       const int64_t gp = (row_base + pair / G) * p.n_q_heads + h * G + pair % G;
@@ -758,11 +774,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
                 make_ushort4(f32_to_bf16(y[0] * inv), f32_to_bf16(y[1] * inv), f32_to_bf16(y[2] * inv),
                              f32_to_bf16(y[3] * inv));
           else
-            *reinterpret_cast<f32x4 *>(p.part_o + ((int64_t)slot * kPairs + j0) * D + e) = y * unit;
+            *reinterpret_cast<f32x4 *>(p.part_o + ((int64_t)slot * kPairs + row_at) * D + e) = y * unit;
         }
       if (hh == 0) {
         if (!whole)
-          p.part_ml[(int64_t)slot * kPairs + j0] = make_float2(m, l);
+          p.part_ml[(int64_t)slot * kPairs + row_at] = make_float2(m, l);
         else if (p.lse_out)
           p.lse_out[gp] = l == 0.f ? kNegInf : (m + __log2f(l)) * kLn2;
       }
@@ -799,17 +815,17 @@ void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStre
 }  // namespace
 
 // Whether a block takes kBytePairs pairs.  Such a block reads and decodes its keys once, but takes
-// 13 us for its first tile and is at work on one CU alone; blocks of 32 pairs read the cache again
-// for every 32, and spread over the chip.  4 KV heads, blocks of 32 and of 256 pairs, in us, D = 128:
+// 10 us for its first tile and its end, and is at work on one CU alone; blocks of 32 pairs read the cache
+// again for every 32, and spread over the chip.  4 KV heads, blocks of 32 and of 256 pairs, in us, D = 128:
 //   sequences x keys     64 pairs     128         256         512
 //   1 x 8,192            16   20      21   24     27   31     37   34
-//   1 x 65,536           34   45      48   49     80   57    143   89
-//   8 x 4,096            26   30      38   36     61   47     93   59
-//   64 x 4,096          107  126     147  139    285  162    534  320
-//   256 x 512            60   78     103   88    198  111    404  221
-// and D = 64: 64 x 4,096 keys with 128 pairs 87 and 107, 256 pairs 155 and 119; 256 x 512: 58 and
-// 65, 110 and 76.  Short caches that leave CUs idle go to blocks of 32 (1 x 1,024 keys with 512
-// pairs 16 and 37).
+//   1 x 65,536           33   34      48   38     80   56    143   92
+//   8 x 4,096            25   26      38   31     61   47     93   60
+//   64 x 4,096           82   90     147  104    285  167    534  327
+//   256 x 512            60   61     103   73    198  113    404  226
+// and D = 64: 64 x 4,096 keys with 128 pairs 86 and 88, 256 pairs 155 and 117; 256 x 512 with 96 pairs
+// 44 and 53, 256 pairs 110 and 75.  Short caches that leave CUs idle go to blocks of 32 (1 x 1,024 keys with
+// 512 pairs 16 and 37).
 inline bool many_pairs(int64_t n_seqs, int64_t n_kv_heads, int64_t n_ctx, int head_dim, int64_t pairs, bool bf16) {
   return bf16 && pairs > (head_dim == 128 ? 64 : 128) &&
          n_seqs * n_kv_heads * ((pairs + 31) / 32) > ((1 << 18) - 1) / std::max<int64_t>(n_ctx, 1);
