@@ -291,8 +291,9 @@ void append_byte_kernel(ByteAppendParams a, int window, int n_runs, int n_brief,
     wave_lds_fence();
     if (member) atomicMax(&rows[x.out ? 0 : at & (kByteBlock - 1)], i);
     wave_lds_fence();
-    if (!x.out && !__ballot(live && lane > first && !member) && rows[kByteBlock - 1] < 0) {
-      // no other row among these 64: the run may go on behind them
+    if (!x.out && !__ballot(live && lane > first && !member)) {
+      // no other row among these 64: the run may go on behind them (also one that has its last token, which
+      // a later row may have again)
       const int end = min((int64_t)(x.seq + 1) * r, (int64_t)p.n);
       for (int base = row0 + 64; base < end; base += 256) {
         int y[4];
