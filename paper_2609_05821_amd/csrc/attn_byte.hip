@@ -373,7 +373,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
 //                   so small that e would leave fp32 (at > m + kFar) at is m + kFar: weights of such
 //                   a block, below 2^(kManySlack - kFar), are 0 in fp16 either way.
 // Both maxima move when a step exceeds them by more than kManySlack: weights stay below
-// 2^(kHead + kManySlack) = 2^15, and sums lose nothing.
+// 2^(kHead + kManySlack) = 2^15, and sums lose nothing.  That M and m stand for the same score to a fraction of a
+// weight's rounding needs them to be small: scores beyond kNear are counted from the largest one (`base`).
 //
 // A step of 32 keys is 2 C slots of one product each, with a share of the vector work of the
 // softmax (of the scores computed one step before), an operand read from LDS for C slots
@@ -399,6 +400,10 @@ constexpr int kManyPad = 6;
 constexpr int kRing = 4;                             // tiles in LDS
 constexpr float kHead = 11.f, kManySlack = 4.f;      // weights stay below 2^(kHead + kManySlack)
 constexpr float kFar = 89.f;
+// Running maxima up to which scores are taken as they are: M_head and at, which have a scale's exponent of up to 119
+// added, are then off by 2^-14 at most, 2^-14.5 of a weight.  (At 2^24 they had been off by 2: beside blocks of other
+// scales a weight came to 4 times what it was, from 2^26 on some were infinite.)
+constexpr float kNear = 1024.f;
 
 __device__ __forceinline__ u32x4 half8(uint32_t lo, uint32_t hi) {
   const f16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false),
@@ -591,9 +596,26 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
 #pragma unroll
       for (int b = 0; b < 2; ++b) x.at[b] = fminf(M_head - sv[b], m_far);
     };
+    // Where a lane's scores are counted from, 0 until a maximum of some lane leaves [-kNear, kNear].  From then on
+    // every step is put over it, and it follows the largest score, so that maxima stay small numbers.
+    float base = 0.f;
+    int look_from = least;  // (first key that some row does not see, or below 0: look at every step)
+    auto put_over_base = [&](Scores &x, const float (&sv)[2]) __attribute__((always_inline)) {
+      const float top = half_max(fmaxf(x.top[0], x.top[1])), by = (top - base) * p.scale_log2;
+      if (by > m_high) {  // (no key yet: top is -inf)
+        set_maxima(m - by, M - by);
+        base = top;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x.s[i] -= base;
+      x.top[0] -= base;
+      x.top[1] -= base;
+      compare(x, sv);
+      exponents(x, sv);
+    };
     // Keys that a row does not see, and maxima that rise: sums and outputs follow.
     auto settle = [&](Scores &x, int key0, const float (&sv)[2]) __attribute__((always_inline)) {
-      if (key0 + 32 > least) {
+      if (key0 + 32 > look_from) {
         const int limit = seen - key0 - 4 * hh;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x.s[i] = (i & 3) + 8 * (i >> 2) < limit ? x.s[i] : kNegInf;
@@ -601,8 +623,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
         top_of(x, 1);
         compare(x, sv);
       }
-      if (x.rises) {
+      if (x.rises || look_from < 0) {
         float mx, my;
+        if (look_from >= 0) {
+          largest(x, sv, mx, my);
+          const float mn = fmaxf(m, half_max(mx));
+          if (__any(fabsf(mn) > kNear && mn > kMInit)) look_from = INT32_MIN;
+        }
+        if (look_from < 0) put_over_base(x, sv);
         largest(x, sv, mx, my);
         const float mn = fmaxf(m, half_max(mx)), Mn = fmaxf(M, half_max(my));
         l *= fast_exp2(m - mn);
@@ -760,6 +788,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
     asm volatile("" : "+v"(row_at));
     l += __shfl_xor(l, 32, 64);
     if (j0 < n_pairs) {
+      const float from0 = __builtin_fmaf(base, p.scale_log2, m);  // the maximum, counted from 0
       const int64_t gp = (row_base + pair / G) * p.n_q_heads + h * G + pair % G;
       // What a weight of 1 stands for, in two equal factors: with the smallest value scales 2^-128.
       const float unit = fast_exp2(0.5f * (M - m - kHead)), inv = l == 0.f ? 0.f : unit / l;
@@ -778,9 +807,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
         }
       if (hh == 0) {
         if (!whole)
-          p.part_ml[(int64_t)slot * kPairs + row_at] = make_float2(m, l);
+          p.part_ml[(int64_t)slot * kPairs + row_at] = make_float2(from0, l);
         else if (p.lse_out)
-          p.lse_out[gp] = l == 0.f ? kNegInf : (m + __log2f(l)) * kLn2;
+          p.lse_out[gp] = l == 0.f ? kNegInf : (from0 + __log2f(l)) * kLn2;
       }
     }
     if (!p.n_workers) break;
