@@ -44,8 +44,12 @@ constexpr int kMaxWaves = 2 * kMaxHeads;
 // (100 rows in windows of 2 and of 4: 9 10 and 10 11; 400: 9 11 and 10 12; 1,000: 14 13 and 10 12.)
 constexpr int kWindow = 16, kWindowFew = 4, kWindowLeast = 2;
 constexpr int kWindowFewFrom = 512, kWindowFrom = 2048, kManyFrom = 8192;
-// Rows of a workgroup that turns queries, and from how many rows on.
+// Rows of a workgroup that turns queries, and from how many rows on.  With the most, whose angles fill the LDS
+// of a block's, a launch has fewer than 2^32 threads for all rows, heads and dims that a call takes (up to 0.8 of that);
+// two a workgroup pass it at 2^24 rows of 4 heads, and the launch then leaves queries out without an error.  (2^22
+// rows, 4 heads of 64 each: 2 rows a workgroup 7.0 ms, 16 rows 3.3.)
 constexpr int kQueryRows = 2, kQueryRowsFrom = 512;
+constexpr int kQueryRowsMost = kByteBlock, kQueryRowsMostFrom = 1 << 22;
 
 // A lane's 16 dims of a head: two vectors of 8, which turn together where they are
 // the two halves of pairs (t >= 0: the first of 8 frequencies).
@@ -556,7 +560,7 @@ void launch(const ByteAppendParams &a, hipStream_t s) {
   const RowParams &p = a.rows;
   const bool many = p.n >= kManyFrom;
   const int window = p.n >= kWindowFrom ? kWindow : p.n >= kWindowFewFrom ? kWindowFew : kWindowLeast;
-  const int query_rows = p.n >= kQueryRowsFrom ? kQueryRows : 1;
+  const int query_rows = p.n >= kQueryRowsMostFrom ? kQueryRowsMost : p.n >= kQueryRowsFrom ? kQueryRows : 1;
   const int heads = std::min(p.n_kv_heads, kMaxHeads), groups = (p.n_kv_heads + heads - 1) / heads;
   const int windows = (p.n + window - 1) / window, n_runs = windows * groups;
   const int n_brief = many || window < kWindow ? 0 : windows;
