@@ -845,19 +845,29 @@ void launch_dim(const MxAttnParams &p, const MxAttnShape &sh, bool bf16, hipStre
 
 // Whether a block takes kBytePairs pairs.  Such a block reads and decodes its keys once, but takes
 // 10 us for its first tile and its end, and is at work on one CU alone; blocks of 32 pairs read the cache
-// again for every 32, and spread over the chip.  4 KV heads, blocks of 32 and of 256 pairs, in us, D = 128:
+// again for every 32, and spread over the chip.  4 KV heads, blocks of 32 and of 256 pairs, in us, D = 128 (every
+// row to the last key):
 //   sequences x keys     64 pairs     128         256         512
-//   1 x 8,192            16   20      21   24     27   31     37   34
-//   1 x 65,536           33   34      48   38     80   56    143   92
-//   8 x 4,096            25   26      38   31     61   47     93   60
-//   64 x 4,096           82   90     147  104    285  167    534  327
-//   256 x 512            60   61     103   73    198  113    404  226
-// and D = 64: 64 x 4,096 keys with 128 pairs 86 and 88, 256 pairs 155 and 117; 256 x 512 with 96 pairs
-// 44 and 53, 256 pairs 110 and 75.  Short caches that leave CUs idle go to blocks of 32 (1 x 1,024 keys with
-// 512 pairs 16 and 37).
+//   1 x 8,192            16   18      21   22     26   31     35   34
+//   1 x 16,384           21   20      25   26     32   32     48   40
+//   1 x 65,536           31   33      45   38     74   55    132   86
+//   8 x 2,048                                     23   38     38   43
+//   8 x 4,096            25   25      36   31     38   46     67   59
+//   64 x 4,096           81   90     140  104    271  161    516  314
+//   256 x 512            59   62     102   72    195  109    404  220
+// and D = 64: 64 x 4,096 keys with 128 pairs 91 and 86, 256 pairs 151 and 116; 256 x 512 with 96 pairs
+// 44 and 53, 256 pairs 107 and 76.  So blocks of 256 pairs for calls whose blocks of 32 have 2^18 keys in all, unless
+// those give every CU one, two or three to do by itself, of up to 2^20 keys on all CUs together: 256 blocks of 1,024 keys
+// take 16 us and in blocks of 256 pairs 38 (D = 64: 11 and 29), of 4,096 38 and 46 (26 and 41), 320 of
+// 2,048 37 and 39, of 3,000 52 and 45, 512 of 2,048 38 and 43 (26 and 38), 1,024 of 1,024 43 and 39 (27 and 30).
+// With sequences of all lengths up to these, 0.4 to 1.1 of the time of blocks of 256 pairs.
+// Of fewer than 256 blocks the two are within 1.2 of one another from 2^18 to 2^19 keys in all, blocks of 32 the faster
+// ones with heads of 128 (1 x 8,192 keys with 256 pairs 26 and 31).
 inline bool many_pairs(int64_t n_seqs, int64_t n_kv_heads, int64_t n_ctx, int head_dim, int64_t pairs, bool bf16) {
-  return bf16 && pairs > (head_dim == 128 ? 64 : 128) &&
-         n_seqs * n_kv_heads * ((pairs + 31) / 32) > ((1 << 18) - 1) / std::max<int64_t>(n_ctx, 1);
+  // (fewer than 2^24 blocks, of up to 2^31 keys)
+  const int64_t blocks = n_seqs * n_kv_heads * ((pairs + 31) / 32), of_a_cu = (blocks + 255) / 256;
+  const bool fills = blocks >= 256 && blocks < 1024 && of_a_cu * 256 * n_ctx <= 1 << 20;
+  return bf16 && pairs > (head_dim == 128 ? 64 : 128) && blocks * n_ctx >= 1 << 18 && !fills;
 }
 
 MxAttnShape byte_attn_shape(int32_t n_seqs, int32_t rows_per_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_ctx,
