@@ -622,8 +622,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_byte_many_kernel(MxAttnP
         top_of(x, 0);
         top_of(x, 1);
         compare(x, sv);
+        if (look_from < 0) x.rises = ~0ull;
       }
-      if (x.rises || look_from < 0) {
+      if (__builtin_expect(x.rises != 0, 0)) {  // (one condition a step: with look_from in it 1,638 rows took 1% longer)
         float mx, my;
         if (look_from >= 0) {
           largest(x, sv, mx, my);
