@@ -25,8 +25,8 @@ class Chosen:
         self.ks = torch.full((per, 1, 4), 127, dtype=torch.uint8)
         self.vs = torch.randint(low, high + 1, (per, 1, 4), generator=g).to(torch.uint8)
 
-    def attend(self, x, pos, wide):
-        """Rows of one head.  wide: the cache has room for 2^18 tokens, so that 256 (row, head) pairs are a block."""
+    def attend(self, x, pos, wide, scale=1.0):
+        """Rows of one head, scale times as large logits as x.  wide: the cache has room for 2^18 tokens, so that 256 (row, head) pairs are a block."""
         pools = [t.to(DEV) for t in (self.k, self.v, self.ks, self.vs)]
         table = torch.zeros(1, 4096, dtype=torch.int32)
         table[0, :len(self.k)] = torch.arange(len(self.k))
@@ -34,7 +34,7 @@ class Chosen:
         q = x[:, None, None].expand(len(x), 1, self.d).contiguous()
         o = torch.full(q.shape, 9.0, dtype=q.dtype, device=DEV)
         lse = torch.full(q.shape[:2], 9.0, device=DEV)
-        api.conduit_attn_byte(cache, q.to(DEV), pos.to(DEV), o, lse_out=lse, scale=1.0 / self.d)
+        api.conduit_attn_byte(cache, q.to(DEV), pos.to(DEV), o, lse_out=lse, scale=scale / self.d)
         return o[:, 0].cpu().double(), lse[:, 0].cpu().double()
 
     def factors(self, scales):
@@ -141,4 +141,36 @@ def test_logits_of_every_size(dtype, wide, d, order, sign):
         if wide and dtype == "bf16":
             err = err + 2.0 ** -36 * (p[:, 0] * c.factors(c.vs)[:seen]).max() * code[:seen].sum(0)
         assert ((o[i] - want).abs() <= err).all(), f"row {i}, queries of 2^{int(exponent[i])}"
+        check_lse(lse[i], torch.logsumexp(logits, 0))
+
+
+@pytest.mark.parametrize("dtype,wide", [("bf16", True), ("bf16", False), ("f32", True)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_products_near_the_largest_number(dtype, wide, d, order):
+    """Sums of products up to 2^126.6 of either sign in one row, whose differences are no finite numbers, with scales that
+    make logits of up to 2^28 of them: the output is the mean over the keys with the row's largest."""
+    rows, ctx = 300, 2000
+    c = Chosen(ctx, d, 7, 110, 130)
+    step = torch.arange(c.ks.numel()) * 8 // c.ks.numel()           # keys of -1.5, -1, -0.5, -0, 0, 0.5, 1 and 1.5
+    if order == "falling":
+        step = 7 - step
+    size = torch.tensor([0x3c, 0x38, 0x30, 0, 0, 0x30, 0x38, 0x3c])[step] + 128 * (step < 4)
+    c.k[:] = size.repeat_interleave(16).view(-1, 1, 64, 1).to(torch.uint8)
+    number = B.decoded(c.k)[:, 0, :, 0].flatten()[:ctx]
+    pos = torch.randint(0, ctx, (rows,), generator=torch.Generator().manual_seed(8), dtype=torch.int32)
+    largest = 126 - (6 if d == 64 else 7)                            # 1.5 d x = 2^126.6
+    x = torch.pow(2.0, (largest - torch.arange(rows) % 10).double()) * (1 - 2 * (torch.arange(rows) // 10 % 2))
+    scale = 2.0 ** (27 - largest)
+    o, lse = c.attend(x.to(DT[dtype]), pos, wide, scale)
+    v, code = c.values()
+    for i in range(rows):
+        seen = int(pos[i]) + 1
+        logits = x[i] * scale * number[:seen]
+        p = torch.softmax(logits, 0)[:, None]
+        want = (p * v[:seen]).sum(0)
+        err = bound(want, (p * v[:seen].abs()).sum(0), dtype, wide)
+        if wide and dtype == "bf16":
+            err = err + 2.0 ** -36 * (p[:, 0] * c.factors(c.vs)[:seen]).max() * code[:seen].sum(0)
+        assert ((o[i] - want).abs() <= err).all(), f"row {i}"
         check_lse(lse[i], torch.logsumexp(logits, 0))
