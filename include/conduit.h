@@ -698,9 +698,12 @@ conduit_status conduit_load_byte(const conduit_kv_byte *cache, const int32_t *sr
  * count as NaN or as 0 (appends write none).
  *
  * Accuracy: products and sums are in fp32.  For bf16 tensors the probabilities enter the
- * product with 11 bits or more; where a call has many (row, head) pairs for a KV head,
- * they do so times the factor of their value block, p * 2^(s - 127), and are off by up to
- * 2^-36 of the row's largest such product besides, times their code.
+ * product in two bf16 parts, up to 2^-17 of each off; where a call has many (row, head)
+ * pairs for a KV head, they enter it as one fp16 number times the factor of their value
+ * block, p * 2^(s - 127), up to 2^-11 of each off, and up to 2^-36 of the row's largest such
+ * product besides, times their code.  Which of the two a call takes follows from its
+ * sequences, rows, heads, head_dim and n_ctx alone (more than 64 pairs, 128 of 64 dims, and
+ * caches of a total size), so a larger n_ctx may change results by that much.
  * ------------------------------------------------------------------------ */
 size_t conduit_attn_byte_workspace_bytes(const conduit_kv_byte *cache, int32_t n, int32_t dtype);
 

@@ -18,7 +18,7 @@
 // Bound by memory where there are many rows, by the chain of loads before the first store
 // (positions, page and what the block holds, rows, angles) where there are few.  Measured, 4 KV heads
 // of 128: a prompt of 17,024 bf16 rows with 28 query heads, keys and queries turned, 63 us, 4.7 TB/s
-// (a copy of 4 GiB: 4.5); 65,536 fp32 rows 91 us, 3.7 TB/s; 1,638 rows here and there with their
+// (a copy of 4 GiB: 4.5); 65,536 fp32 rows 92 us, 3.7 TB/s; 1,638 rows here and there with their
 // queries 14 us, 2.0 TB/s; 64 tokens of as many sequences 7 us.
 #include <algorithm>
 #include <cfloat>

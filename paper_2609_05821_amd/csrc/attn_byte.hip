@@ -23,7 +23,7 @@
 // The sum they are divided by is of the fp32 probabilities.
 // Measured (bf16, D = 128): 62 sequences of up to 32,768 tokens, 28 heads over 4, 1.06 GB: 190 us
 // and 5 to merge, 5.5 TB/s (a copy of 4 GiB: 4.5); one of 131,072, 32 heads over 8, 268 MB: 51 and 5;
-// 8 of up to 8,211 with 5 rows, 76 MB: 21 and 5, which is mostly the chain of loads a
+// 8 of up to 8,211 with 5 rows, 76 MB: 22 and 4, which is mostly the chain of loads a
 // workgroup begins with (positions, page, codes) for 4 steps of its own.
 //
 // Many pairs (attn_byte_many_kernel): bound by the matrix products.  See there.
@@ -384,18 +384,20 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, MT, NS)) void attn_byte_k
 //
 // What bounds it: the product of 32 x 32 x 16 takes 13.8 ns a SIMD on zeros and 21 on random
 // numbers (1.6 PFLOP/s: the chip lowers its clock), 27.6 with the vector work that a slot needs here. A
-// tile takes 2.06 us at D = 128 (64 keys, 256 pairs a CU: 1.04 PFLOP/s over the chip) and 1.39 at
-// D = 64.  64 pairs a wave on one wave a SIMD take as long (2.03 to 2.06; 1.50 at D = 64), so do slots that
-// lag the waves behind one another (2.06 to 2.10), and keys and values decoded
-// by every wave for itself take 620 us for 1,638 rows over 17,024 keys where this takes 232.
+// tile takes 1.93 to 2.06 us at D = 128, by the card and its clock (64 keys, 256 pairs a CU: 1.04 to 1.11 PFLOP/s over the
+// chip), and 1.35 to 1.39 at D = 64.  Where it took 2.06, 64 pairs a wave on one wave a SIMD took as long (2.03
+// to 2.06; 1.50 at D = 64), and so did slots that lag the waves behind one another (2.06 to 2.10); keys and values
+// decoded by every wave for itself took 620 us for 1,638 rows over 17,024 keys where this takes 224.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr int kManyWaves = 8;
 constexpr int kManyThreads = 64 * kManyWaves;
 constexpr int kBytePairs = 32 * kManyWaves;          // pairs of a block
 // What beginning a block costs, in tiles: its first tiles and queries, and the rows of the part
-// that it leaves for the merge.  (1,638 rows over 17,024 keys: 1 tile 273 us, 3 242, 6 232, 8 234,
-// 12 237, 16 240; 4 sequences of 333 rows over 4,100 states: 3 95, 6 93, 12 100.)
+// that it leaves for the merge.  With 3, 6, 8 and 12 tiles: 1,638 rows over 17,024 keys, 28 heads over 4, 252 244 245 248
+// us; 4,000 over 8,000, 8 heads over 4, 100 97 99 101; 1,000 over 9,000, 16 over 8, 72 73 73 72; 4 sequences of 333 rows to
+// all of up to 4,100 states, 32 over 8, 107 105 106 109; 7 of 200 to 6,000, 16 over 4, 77 73 75 76; 16 of 100 to
+// 2,500, 32 over 4, 76 74 77 82; 3 of 150 to 20,000, 20 over 4, and 2 of 900 to 5,000, 8 over 8, within 1%.
 constexpr int kManyPad = 6;
 constexpr int kRing = 4;                             // tiles in LDS
 constexpr float kHead = 11.f, kManySlack = 4.f;      // weights stay below 2^(kHead + kManySlack)

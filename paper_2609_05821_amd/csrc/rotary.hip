@@ -503,8 +503,8 @@ hipError_t launch_rows(const RowParams &p, RowMode mode, bool bf16, hipStream_t 
   ProfScope ps(names[mode], s);
   const int half = p.rope.half;
   const int units = p.n_q_heads + p.n_kv_heads;
-  // (fp32 rows loaded from 4 bits: 8 dims a lane let four lanes trade pieces of one
-  // run of dims instead of two; 65,536 rows 58 us, in pairs 71)
+  // (fp32 rows loaded from 4 or 8 bits: 8 dims a lane let four lanes trade pieces of one
+  // run of dims instead of two; 65,536 rows from 4 bits 58 us, in pairs 71)
   const bool pairs = 2 * half == p.head_dim && units > 1 && (bf16 || (mode != kRowLoadMx && mode != kRowLoadByte));
   const HeadShape shape = p.rope.adjacent || !half ? kVectors
                           : half % kVec           ? kSingles
